@@ -31,7 +31,7 @@
  *  - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *    tw_gemm / tw_dense_gemm only enqueue work on it: they never synchronise
  *    and never allocate.
- *  - Inputs are assumed finite.
+ *  - Inputs are assumed finite (the few-bit operators at the end say what others do).
  */
 #ifndef TWGEMM_H
 #define TWGEMM_H
@@ -60,7 +60,7 @@ typedef enum {
 typedef enum { TW_PATTERN_TW = 0, TW_PATTERN_TVW = 1, TW_PATTERN_TEW = 2 } tw_pattern;
 
 /* Element type of a packed weight (and of the A it multiplies). */
-typedef enum { TW_DTYPE_F16 = 0, TW_DTYPE_I8 = 1 } tw_dtype;
+typedef enum { TW_DTYPE_F16 = 0, TW_DTYPE_I8 = 1, TW_DTYPE_MX4 = 2 } tw_dtype;
 
 /*
  * Memory layout of A and C.  Section V ("Memory Accesses Coalesce") stores the
@@ -115,7 +115,9 @@ typedef struct {
   const int32_t* ew_row;
   const uint16_t* ew_val;
   int32_t dtype;               /* TW_DTYPE_I8: every entry of `values` is an int8 value,
-                                  sign-extended to 16 bits; offsets count elements */
+                                  sign-extended to 16 bits; offsets count elements.
+                                  TW_DTYPE_MX4: the fp16 values that the 4-bit blocks stand
+                                  for, row_idx whole blocks of 32 rows */
 } tw_packed_view;
 
 /*
@@ -358,6 +360,77 @@ tw_status tw_conv_free(tw_conv_t binding);
 tw_status tw_conv_gemm(const void* X_dev, tw_conv_t binding, void* C_dev, int ldc, void* stream);
 tw_status tw_conv_gemm_i8(const void* X_dev, tw_conv_t binding, void* C_dev, int ldc, int c_dtype,
                           float scale, void* stream);
+
+/*
+ * Few-bit layers: what makes the 8- and 4-bit operands of the products from fp16 activations, and the products that
+ * give fp16 back, so that a pruned layer runs in 8 or 4 bits between fp16 activations.
+ *
+ * Common to the calls below: activations are K x M (token m of row k at X[k*ld + m], TW_LAYOUT_KM), device memory, 16-byte
+ * aligned; the scales of tw_rmsnorm / tw_quant_i8 / tw_gemm_i8_scaled are 4-byte aligned.  Columns M .. ld-1 are never
+ * written; they may be read (whatever they hold) and have to be readable.  M <= 2^27 (the 4-bit calls: ldq <= 2^27) and
+ * K <= 131071, else TW_ERR_UNSUPPORTED.  Asynchronous on `stream`, allocate nothing, keep no state between calls.
+ * Unlike elsewhere in this library an infinity or NaN is an allowed input of the norm and the quantisers: it marks its token
+ * (its block of a token) as said there and reaches no other.
+ *
+ * tw_rmsnorm - residual sum, root-mean-square norm over the K values of every token, output in int8 and / or fp16:
+ *     h = fp16(x + r);  g = h * gamma[k];  inv = 1 / sqrt(mean_k(h^2) + eps)
+ *     Y = fp16(g * inv);   scale[m] = max_k|g| * inv / 127;   Q = round-half-even(127 g / max_k|g|)
+ *   Q is that integer exactly (in [-127, 127]); sums and scales are fp32.  A token of zeros: scale 0, Q 0.  A token with an
+ *   infinity or NaN among h or g: scale NaN, Q 0 (Y by the formula).
+ *   X_dev     fp16, ld >= M, multiple of 8;  R_dev  the residual, same ld, or NULL (h = x)
+ *   gamma_dev K fp16 factors or NULL (ones);  eps > 0, finite
+ *   H_dev     receives h, same ld, or NULL; only with R_dev; may be X_dev or R_dev itself
+ *   Y_dev     fp16 output, same ld, or NULL
+ *   Q_dev, scale_dev  int8 K x M (ldq >= M, multiple of 16: the operand of tw_gemm_i8 / tw_gemm_i8_scaled) and M floats; or
+ *             both NULL.  One of Y_dev and Q_dev is needed.
+ *   Outputs must not overlap anything else.  Errors: TW_ERR_ARG, TW_ERR_UNSUPPORTED, TW_ERR_HIP.
+ * tw_quant_i8 - the int8 output alone, of activations as they are: scale[m] = max_k|x| / 127, Q as above.
+ *
+ * tw_gemm_i8_scaled - tw_gemm_i8 whose output is fp16 in real units:
+ *     C[n][m] = fp16( fp32(sum) * (a_scale[m] * w_scale[n]) ),  every step one rounding
+ *   a_scale_dev M floats (of the tokens), w_scale_dev N floats (of the weight's columns); C_dev fp16, ldc >= M, multiple of
+ *   8; pruned columns are +0.  A, M, lda, the handle and the errors as tw_gemm_i8.
+ *
+ * Microscaled 4-bit floating point (TW_DTYPE_MX4).  32 consecutive rows of a column (of a token) are a block: 32 codes
+ * of e2m1 (sign, 2 bits exponent, 1 bit mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one scale byte s, a factor 2^(s-127).
+ *     s - 127 = floor(log2(max|x|)) - 2;  value = x / 2^(s-127) to the nearest, ties to the even code, past 6 to 6
+ *   (exact powers of two: there is one right result, and tests compare bits).  A block of zeros: s = 127; of a
+ *   token with an infinity or NaN in it: s = 255 (NaN), codes 0.  The last block of a K that is no multiple of 32 is
+ *   filled up with zeros.
+ *
+ * tw_quant_mx4 - activations to that form.  With nb = ceil(K/32) and ldq >= M, a multiple of 16:
+ *   X_dev  fp16; layout TW_LAYOUT_KM (ldx >= M) or TW_LAYOUT_MK (row-major, X[m*ldx + k], ldx >= K); ldx multiple of 8
+ *   Q_dev  nb * ldq * 16 bytes: the codes of block b of token m at (b*ldq + m)*16, row 32b + 2i in the low half of byte i
+ *          and row 32b + 2i + 1 in the high half
+ *   S_dev  nb * ldq bytes: its scale byte at b*ldq + m
+ *   Errors: TW_ERR_ARG, TW_ERR_UNSUPPORTED, TW_ERR_HIP.
+ * tw_pack_mx4_host / tw_pack_mx4 - as tw_pack_host / tw_pack, for any mask: columns without a kept element are dropped, the
+ *   others cut into tiles of G (64 or 128; 32: TW_ERR_UNSUPPORTED), and a tile drops the blocks of 32 rows in which it keeps
+ *   nothing; a block that it keeps in part is stored with zeros.  The kept weights are quantised (TW_ERR_ARG if one is not
+ *   finite); weights that came out of this format come back unchanged.  The handle works with tw_upload, tw_concat, tw_export
+ *   and tw_unpack (the values that the blocks stand for, fp16, exact; the mask of the kept blocks), tw_flop_counts and
+ *   tw_free; the other products and tw_conv_bind refuse it.
+ * tw_gemm_mx4 - C = A . W over the blocks that a tile keeps: fp32 sums, one rounding to fp16.  C_dev fp16 N x M, ldc >= M,
+ *   multiple of 8; pruned columns are +0, also those of a token with a NaN block, whose other columns are NaN where their tile
+ *   keeps that block.  Errors: as tw_gemm; TW_ERR_STATE also on another device than the handle's.
+ * tw_gemm_mx4_grouped - products grouped by expert: h from tw_concat of E weights of the same N (a handle that was not
+ *   concatenated is one expert; members of different N: TW_ERR_ARG).  Expert e multiplies the tokens offsets[e] ..
+ *   offsets[e+1]-1, and C is N x M with the N of one expert.  offsets_dev: E+1 int32 on the device, ascending, in [0, M]; nothing
+ *   about them is known to the host, no call waits for them.  An expert without tokens costs little; columns of C that belong
+ *   to no expert (in front of offsets[0], from offsets[E] on) are left as they were.  Offsets outside [0, M] are cut to it and
+ *   an end in front of its start is no tokens; nothing outside the M columns is touched whatever they hold.
+ */
+tw_status tw_rmsnorm(const void* X_dev, const void* R_dev, const void* gamma_dev, float eps, int M, int K, int ld,
+                     void* H_dev, void* Y_dev, void* Q_dev, int ldq, float* scale_dev, void* stream);
+tw_status tw_quant_i8(const void* X_dev, int M, int K, int ldx, void* Q_dev, int ldq, float* scale_dev, void* stream);
+tw_status tw_gemm_i8_scaled(const void* A_dev, int M, int lda, tw_handle_t h, const float* a_scale_dev,
+                            const float* w_scale_dev, void* C_dev, int ldc, void* stream);
+tw_status tw_quant_mx4(const void* X_dev, int M, int K, int ldx, int layout, void* Q_dev, void* S_dev, int ldq, void* stream);
+tw_status tw_pack_mx4_host(const uint16_t* B_host, const uint8_t* mask_host, int K, int N, int G, tw_handle_t* out);
+tw_status tw_pack_mx4(const uint16_t* B_host, const uint8_t* mask_host, int K, int N, int G, tw_handle_t* out);
+tw_status tw_gemm_mx4(const void* Q_dev, const void* S_dev, int M, int ldq, tw_handle_t h, void* C_dev, int ldc, void* stream);
+tw_status tw_gemm_mx4_grouped(const void* Q_dev, const void* S_dev, int M, int ldq, const int32_t* offsets_dev, tw_handle_t h,
+                              void* C_dev, int ldc, void* stream);
 
 /* tw_export - fill *out with the logical view (host pointers owned by h). */
 tw_status tw_export(tw_handle_t h, tw_packed_view* out);

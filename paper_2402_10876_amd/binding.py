@@ -15,13 +15,14 @@ import numpy as np
 
 PATTERN_TW, PATTERN_TVW, PATTERN_TEW = 0, 1, 2
 LAYOUT_KM, LAYOUT_MK = 0, 1
-DTYPE_F16, DTYPE_I8 = 0, 1
+DTYPE_F16, DTYPE_I8, DTYPE_MX4 = 0, 1, 2
 
 EXPORTED_SYMBOLS = [
     "tw_pack_host", "tw_upload", "tw_pack", "tw_pack_dev", "tw_prune_dev",
     "tw_prune_workspace_bytes", "tw_prune_dev_static", "tw_concat", "tw_gemm", "tw_dense_gemm", "tw_export",
     "tw_unpack", "tw_free", "tw_status_str", "tw_set_option", "tw_flop_counts",
     "tw_pack_i8_host", "tw_pack_i8", "tw_gemm_i8", "tw_dense_gemm_i8", "tw_conv_bind", "tw_conv_free", "tw_conv_gemm", "tw_conv_gemm_i8", "tw_calibrate",
+    "tw_rmsnorm", "tw_quant_i8", "tw_gemm_i8_scaled", "tw_quant_mx4", "tw_pack_mx4_host", "tw_pack_mx4", "tw_gemm_mx4", "tw_gemm_mx4_grouped",
     "tw_gemm_ex", "tw_launch_opts_init", "tw_gemm_workspace_bytes", "tw_workspace_init",
 ]
 
@@ -118,6 +119,14 @@ def lib():
         L.tw_launch_opts_init.argtypes = [C.POINTER(LaunchOpts)]
         L.tw_gemm_workspace_bytes.argtypes = [vp, i, C.POINTER(C.c_size_t)]
         L.tw_workspace_init.argtypes = [vp, C.c_size_t, vp]
+        L.tw_rmsnorm.argtypes = [vp, vp, vp, C.c_float, i, i, i, vp, vp, vp, i, vp, vp]
+        L.tw_quant_i8.argtypes = [vp, i, i, i, vp, i, vp, vp]
+        L.tw_gemm_i8_scaled.argtypes = [vp, i, i, vp, vp, vp, vp, i, vp]
+        L.tw_quant_mx4.argtypes = [vp, i, i, i, i, vp, vp, i, vp]
+        L.tw_pack_mx4_host.argtypes = [vp, vp, i, i, i, C.POINTER(vp)]
+        L.tw_pack_mx4.argtypes = L.tw_pack_mx4_host.argtypes
+        L.tw_gemm_mx4.argtypes = [vp, vp, i, i, vp, vp, i, vp]
+        L.tw_gemm_mx4_grouped.argtypes = [vp, vp, i, i, vp, vp, vp, i, vp]
         L.tw_conv_gemm.argtypes = [vp, vp, vp, i, vp]
         L.tw_conv_gemm_i8.argtypes = [vp, vp, vp, i, i, C.c_float, vp]
         L.tw_calibrate.argtypes = [i, vp, vp, C.c_size_t, i, vp, C.POINTER(C.c_double)]
@@ -288,6 +297,28 @@ def tw_pack_i8(B8, mask, G, pattern=PATTERN_TW, tile_mask=None) -> PackedWeight:
     return _pack_i8("tw_pack_i8", B8, mask, G, pattern, tile_mask)
 
 
+def _pack_mx4(fn_name, B16, mask, G):
+    B16 = np.ascontiguousarray(B16)
+    if B16.dtype != np.float16 and B16.dtype != np.uint16:
+        raise TypeError("B must be fp16 (or its uint16 bit patterns)")
+    mask = np.ascontiguousarray(mask, dtype=np.uint8)
+    if mask.shape != B16.shape or B16.ndim != 2:
+        raise ValueError("B and mask must be K x N")
+    K, N = B16.shape
+    h = C.c_void_p()
+    _check(getattr(lib(), fn_name)(_host_ptr(B16), _host_ptr(mask), K, N, int(G), C.byref(h)), fn_name)
+    return PackedWeight(h)
+
+
+def tw_pack_mx4_host(B16, mask, G) -> PackedWeight:
+    """fp16 weight and any mask to microscaled 4-bit blocks of 32 rows (tiles of G kept columns drop whole blocks)."""
+    return _pack_mx4("tw_pack_mx4_host", B16, mask, G)
+
+
+def tw_pack_mx4(B16, mask, G) -> PackedWeight:
+    return _pack_mx4("tw_pack_mx4", B16, mask, G)
+
+
 def tw_prune_workspace_bytes(K: int, N: int, G: int) -> int:
     n = C.c_size_t()
     _check(lib().tw_prune_workspace_bytes(K, N, G, C.byref(n)), "tw_prune_workspace_bytes")
@@ -355,6 +386,40 @@ def tw_dense_gemm_i8(A_ptr: int, B_ptr: int, C_ptr: int, M: int, K: int, N: int,
                      ldc: int, c_dtype: int = 0, scale: float = 1.0, stream: int = 0):
     _check(lib().tw_dense_gemm_i8(A_ptr, B_ptr, C_ptr, M, K, N, lda, ldb, ldc, c_dtype, scale, stream),
            "tw_dense_gemm_i8")
+
+
+def tw_rmsnorm(X_ptr: int, R_ptr, gamma_ptr, eps: float, M: int, K: int, ld: int, H_ptr, Y_ptr, Q_ptr, ldq: int, scale_ptr,
+               stream: int = 0):
+    """Residual sum, root-mean-square norm, output in int8 with a scale per token and / or in fp16; addresses that may be
+    None: R, gamma, H, Y, and Q with scale (see include/twgemm.h)."""
+    _check(lib().tw_rmsnorm(X_ptr, R_ptr, gamma_ptr, eps, M, K, ld, H_ptr, Y_ptr, Q_ptr, ldq, scale_ptr, stream), "tw_rmsnorm")
+
+
+def tw_quant_i8(X_ptr: int, M: int, K: int, ldx: int, Q_ptr: int, ldq: int, scale_ptr: int, stream: int = 0):
+    """fp16 activations (K x M) to int8 with a scale per token."""
+    _check(lib().tw_quant_i8(X_ptr, M, K, ldx, Q_ptr, ldq, scale_ptr, stream), "tw_quant_i8")
+
+
+def tw_gemm_i8_scaled(A_ptr: int, M: int, lda: int, packed: PackedWeight, a_scale_ptr: int, w_scale_ptr: int, C_ptr: int,
+                      ldc: int, stream: int = 0):
+    """int8 A times a packed int8 weight; C (N x M) fp16 = sums * a_scale (of the token) * w_scale (of the column)."""
+    _check(lib().tw_gemm_i8_scaled(A_ptr, M, lda, packed.handle, a_scale_ptr, w_scale_ptr, C_ptr, ldc, stream), "tw_gemm_i8_scaled")
+
+
+def tw_quant_mx4(X_ptr: int, M: int, K: int, ldx: int, layout: int, Q_ptr: int, S_ptr: int, ldq: int, stream: int = 0):
+    """fp16 activations to microscaled 4-bit blocks: codes (ceil(K/32) x ldq x 16 bytes) and scale bytes (ceil(K/32) x ldq)."""
+    _check(lib().tw_quant_mx4(X_ptr, M, K, ldx, layout, Q_ptr, S_ptr, ldq, stream), "tw_quant_mx4")
+
+
+def tw_gemm_mx4(Q_ptr: int, S_ptr: int, M: int, ldq: int, packed: PackedWeight, C_ptr: int, ldc: int, stream: int = 0):
+    """4-bit activations times a 4-bit weight; C (N x M) fp16."""
+    _check(lib().tw_gemm_mx4(Q_ptr, S_ptr, M, ldq, packed.handle, C_ptr, ldc, stream), "tw_gemm_mx4")
+
+
+def tw_gemm_mx4_grouped(Q_ptr: int, S_ptr: int, M: int, ldq: int, offsets_ptr: int, packed: PackedWeight, C_ptr: int, ldc: int,
+                        stream: int = 0):
+    """The same by expert: tokens offsets[e] .. offsets[e+1]-1 (int32 on the device) meet member e of a tw_concat handle."""
+    _check(lib().tw_gemm_mx4_grouped(Q_ptr, S_ptr, M, ldq, offsets_ptr, packed.handle, C_ptr, ldc, stream), "tw_gemm_mx4_grouped")
 
 
 class ConvBinding:

@@ -3,10 +3,12 @@
 #include <hip/hip_runtime_api.h>
 
 #include <atomic>
+#include <cfloat>
 #include <cstring>
 #include <new>
 #include <vector>
 
+#include "fewbit.h"
 #include "kernels.h"
 #include "packed.h"
 #include "prune.h"
@@ -64,6 +66,9 @@ bool automatic(const Opts& o) {
 // Workspace of the K split across workgroups: 1024 counters, then the fp32 partial tiles.
 constexpr size_t WS_COUNTER_BYTES = 4096;
 constexpr int WS_MAX_PAIRS = (int)(WS_COUNTER_BYTES / 4);
+
+// Tokens of a call of the few-bit operators: grids of one dimension, and 16 bytes per token in 32 bits.
+constexpr int MOST_TOKENS = 1 << 27;
 
 bool valid_G(int G) { return G == 32 || G == 64 || G == 128; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -251,12 +256,42 @@ tw_status tw_pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* ti
   return TW_OK;
 }
 
+// The parts of a microscaled 4-bit image in one allocation, 256-byte aligned each.
+static tw_status upload_mx4(tw_handle_t h, int dev) {
+  twg::Mx4Image& d = h->mx4;
+  const void* src[7] = {d.tiles.data(), d.member_tile.data(), d.member_col.data(), d.blocks.data(), d.col_idx.data(),
+                        d.zero_cols.data(), d.vals.data()};
+  const size_t bytes[7] = {d.tiles.size() * sizeof(twg::Mx4Tile), d.member_tile.size() * 4, d.member_col.size() * 4,
+                           d.blocks.size() * 2, d.col_idx.size() * 4, d.zero_cols.size() * 4, d.vals.size()};
+  size_t total = 0;
+  for (int i = 0; i < 7; ++i) {
+    d.off[i] = total;
+    total += (bytes[i] + 255) / 256 * 256;
+  }
+  d.off_scales = total;
+  total += (d.scales.size() + 255) / 256 * 256;
+  void* blob = nullptr;
+  if (hipMalloc(&blob, total) != hipSuccess) { (void)hipGetLastError(); return TW_ERR_ALLOC; }
+  bool ok = d.scales.empty() ||
+            hipMemcpy((char*)blob + d.off_scales, d.scales.data(), d.scales.size(), hipMemcpyHostToDevice) == hipSuccess;
+  for (int i = 0; ok && i < 7; ++i)
+    ok = !bytes[i] || hipMemcpy((char*)blob + d.off[i], src[i], bytes[i], hipMemcpyHostToDevice) == hipSuccess;
+  if (!ok) {
+    (void)hipGetLastError();
+    (void)hipFree(blob);
+    return TW_ERR_HIP;
+  }
+  h->img.blob = blob; h->img.blob_bytes = total; h->img.device = dev;
+  return TW_OK;
+}
+
 tw_status tw_upload(tw_handle_t h) {
   if (!h) return TW_ERR_ARG;
   twg::DeviceImage& d = h->img;
   if (d.blob) return TW_OK;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
+  if (h->dtype == TW_DTYPE_MX4) return upload_mx4(h, dev);
   twg::ImageLayout L;
   twg::layout_image(h, &L);
   const void* src[twg::IMG_PARTS] = {};
@@ -571,7 +606,7 @@ tw_status tw_conv_bind(tw_handle_t h, const tw_conv_geom* cg, int64_t ldx, tw_co
   const int chunk = h->dtype == TW_DTYPE_I8 ? 16 : 8;          // elements per 16-byte copy
   const int64_t reach = (Mp + chunk - 1) / chunk * chunk + (int64_t)(cg->R - 1) * cg->P + cg->S - 1;
   if (ldx < reach || ldx % chunk || (int64_t)cg->C * ldx >= (1ll << 31)) return TW_ERR_ARG;
-  if (h->pattern == TW_PATTERN_TEW || h->G == 32) return TW_ERR_UNSUPPORTED;
+  if (h->pattern == TW_PATTERN_TEW || h->G == 32 || h->dtype == TW_DTYPE_MX4) return TW_ERR_UNSUPPORTED;
   if (!h->img.blob) return TW_ERR_STATE;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
@@ -676,11 +711,12 @@ static int pick_tile_m_i8(const Opts& o, int M, int n_tiles, int G, int max_k) {
 
 // The launch behind tw_gemm_i8 and tw_conv_gemm_i8 (conv: see gemm_launch).
 static tw_status gemm_i8_launch(const void* A, int M, int lda, tw_handle_t h, void* C, int ldc, int c_dtype,
-                                float scale, void* stream, const tw_conv_s* conv) {
+                                float scale, void* stream, const tw_conv_s* conv, const float* a_scale = nullptr,
+                                const float* w_scale = nullptr) {
   const Opts o = default_opts();
   twg::GemmI8Args g{};
   g.A = (const int8_t*)A; g.C = C; g.M = M; g.lda = lda; g.ldc = ldc;
-  g.c_i8 = c_dtype; g.scale = scale;
+  g.c_dtype = c_dtype; g.scale = scale; g.a_scale = a_scale; g.w_scale = w_scale;
   g.vals = (const int8_t*)h->img.d_vals;
   g.row_idx = h->img.d_row_idx; g.col_idx = h->img.d_col_idx; g.tile_sched = h->img.d_tile_sched;
   g.uniform_kp = h->img.uniform_kp;
@@ -731,6 +767,17 @@ tw_status tw_gemm_i8(const void* A, int M, int lda, tw_handle_t h, void* C, int 
   return gemm_i8_launch(A, M, lda, h, C, ldc, c_dtype, scale, stream, nullptr);
 }
 
+tw_status tw_gemm_i8_scaled(const void* A, int M, int lda, tw_handle_t h, const float* a_scale, const float* w_scale,
+                            void* C, int ldc, void* stream) {
+  if (!A || !C || !h || !a_scale || !w_scale || M < 1) return TW_ERR_ARG;
+  if (!aligned16(A) || !aligned16(C) || lda % 16 || ldc % 8 || lda < M || ldc < M) return TW_ERR_ARG;
+  if (((uintptr_t)a_scale & 3) || ((uintptr_t)w_scale & 3) || h->dtype != TW_DTYPE_I8) return TW_ERR_ARG;
+  if (!h->img.blob) return TW_ERR_STATE;
+  if (h->G == 32 || h->K > 131071) return TW_ERR_UNSUPPORTED;
+  if ((unsigned long long)h->K * (unsigned long long)lda >= (1ull << 32)) return TW_ERR_UNSUPPORTED;
+  return gemm_i8_launch(A, M, lda, h, C, ldc, 2, 0.f, stream, nullptr, a_scale, w_scale);
+}
+
 tw_status tw_conv_gemm_i8(const void* X, tw_conv_t b, void* C, int ldc, int c_dtype, float scale,
                           void* stream) {
   if (!X || !C || !b || !b->h || (c_dtype != 0 && c_dtype != 1)) return TW_ERR_ARG;
@@ -752,7 +799,7 @@ tw_status tw_dense_gemm_i8(const void* A, const void* B, void* C, int M, int K, 
     return TW_ERR_UNSUPPORTED;
   twg::GemmI8Args g{};
   g.A = (const int8_t*)A; g.C = C; g.M = M; g.lda = lda; g.ldc = ldc;
-  g.c_i8 = c_dtype; g.scale = scale;
+  g.c_dtype = c_dtype; g.scale = scale;
   g.vals = (const int8_t*)B; g.ldb = ldb; g.K = K; g.N = N;
   const int tn = 128;
   g.n_tiles = (N + tn - 1) / tn;
@@ -761,6 +808,96 @@ tw_status tw_dense_gemm_i8(const void* A, const void* B, void* C, int M, int K, 
   hipError_t e = twg::launch_dense_i8(tn, pick_tile_m_i8(o, M, g.n_tiles, tn, K), g, (hipStream_t)stream);
   if (e == hipErrorInvalidValue) return TW_ERR_UNSUPPORTED;
   return e == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+tw_status tw_rmsnorm(const void* X, const void* R, const void* gamma, float eps, int M, int K, int ld, void* H, void* Y,
+                     void* Q, int ldq, float* scale, void* stream) {
+  if (!X || M < 1 || K < 1 || ld < M || ld % 8 || !(eps > 0.f) || eps > FLT_MAX) return TW_ERR_ARG;
+  if ((!Y && !Q) || !Q != !scale || (H && !R)) return TW_ERR_ARG;
+  if (!aligned16(X) || !aligned16(R) || !aligned16(H) || !aligned16(Y) || !aligned16(Q)) return TW_ERR_ARG;
+  if (((uintptr_t)gamma & 1) || ((uintptr_t)scale & 3) || (Q && (ldq < M || ldq % 16))) return TW_ERR_ARG;
+  if (M > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  const twg::NormArgs g{(const _Float16*)X, (const _Float16*)R, (const _Float16*)gamma, (_Float16*)H, (_Float16*)Y, (int8_t*)Q,
+                        scale, M, K, ld, ldq, eps};
+  return twg::launch_norm(true, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+tw_status tw_quant_i8(const void* X, int M, int K, int ldx, void* Q, int ldq, float* scale, void* stream) {
+  if (!X || !Q || !scale || M < 1 || K < 1 || ldx < M || ldx % 8 || ldq < M || ldq % 16) return TW_ERR_ARG;
+  if (!aligned16(X) || !aligned16(Q) || ((uintptr_t)scale & 3)) return TW_ERR_ARG;
+  if (M > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  const twg::NormArgs g{(const _Float16*)X, nullptr, nullptr, nullptr, nullptr, (int8_t*)Q, scale, M, K, ldx, ldq, 0.f};
+  return twg::launch_norm(false, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+tw_status tw_quant_mx4(const void* X, int M, int K, int ldx, int layout, void* Q, void* S, int ldq, void* stream) {
+  if (!X || !Q || !S || M < 1 || K < 1 || ldx % 8 || ldq < M || ldq % 16) return TW_ERR_ARG;
+  if (layout != TW_LAYOUT_KM && layout != TW_LAYOUT_MK) return TW_ERR_ARG;
+  if (ldx < (layout == TW_LAYOUT_KM ? M : K)) return TW_ERR_ARG;
+  if (!aligned16(X) || !aligned16(Q) || !aligned16(S)) return TW_ERR_ARG;
+  if (ldq > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  const twg::QuantMx4Args g{(const _Float16*)X, (uint8_t*)Q, (uint8_t*)S, M, K, ldx, ldq};
+  return twg::launch_quant_mx4(layout == TW_LAYOUT_KM, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+tw_status tw_pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_t* out) {
+  if (!out) return TW_ERR_ARG;
+  *out = nullptr;
+  if (!B || !mask || K < 1 || N < 1 || !valid_G(G)) return TW_ERR_ARG;
+  if (G == 32 || K > 131071) return TW_ERR_UNSUPPORTED;
+  tw_handle_s* h = new (std::nothrow) tw_handle_s();
+  if (!h) return TW_ERR_ALLOC;
+  const tw_status st = twg::pack_mx4_host(B, mask, K, N, G, h);
+  if (st != TW_OK) { delete h; return st; }
+  *out = h;
+  return TW_OK;
+}
+
+tw_status tw_pack_mx4(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_t* out) {
+  tw_status st = tw_pack_mx4_host(B, mask, K, N, G, out);
+  if (st != TW_OK) return st;
+  st = tw_upload(*out);
+  if (st != TW_OK) { tw_free(*out); *out = nullptr; }
+  return st;
+}
+
+// The launch behind tw_gemm_mx4 and tw_gemm_mx4_grouped.
+static tw_status gemm_mx4_launch(const void* Q, const void* S, int M, int ldq, const int32_t* offsets, tw_handle_t h, void* C,
+                                 int ldc, void* stream) {
+  if (!Q || !S || !C || !h || M < 1 || ldq < M || ldq % 16 || ldc < M || ldc % 8) return TW_ERR_ARG;
+  if (!aligned16(Q) || !aligned16(S) || !aligned16(C) || h->dtype != TW_DTYPE_MX4) return TW_ERR_ARG;
+  if (!h->img.blob) return TW_ERR_STATE;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
+  if (dev != h->img.device) return TW_ERR_STATE;
+  if (ldq > MOST_TOKENS) return TW_ERR_UNSUPPORTED;
+  const twg::Mx4Image& d = h->mx4;
+  const char* p = (const char*)h->img.blob;
+  twg::GemmMx4Args g{};
+  g.Q = (const uint8_t*)Q; g.S = (const uint8_t*)S; g.C = (_Float16*)C; g.M = M; g.ldq = ldq; g.ldc = ldc;
+  g.tiles = (const twg::Mx4Tile*)(p + d.off[0]);
+  g.member_tile = (const int32_t*)(p + d.off[1]); g.member_col = (const int32_t*)(p + d.off[2]);
+  g.blocks = (const uint16_t*)(p + d.off[3]);
+  g.col_idx = (const int32_t*)(p + d.off[4]); g.zero_cols = (const int32_t*)(p + d.off[5]);
+  g.vals = (const uint8_t*)(p + d.off[6]); g.wscale = (const uint8_t*)(p + d.off_scales);
+  g.offsets = offsets;
+  g.n_members = offsets ? (int)d.member_tile.size() - 1 : 1;
+  g.n_tiles = offsets ? d.max_member_tiles : (int)d.tiles.size();
+  const hipError_t e = twg::launch_gemm_mx4(h->G, g, (hipStream_t)stream);
+  if (e == hipErrorInvalidValue) return TW_ERR_UNSUPPORTED;
+  return e == hipSuccess ? TW_OK : TW_ERR_HIP;
+}
+
+tw_status tw_gemm_mx4(const void* Q, const void* S, int M, int ldq, tw_handle_t h, void* C, int ldc, void* stream) {
+  return gemm_mx4_launch(Q, S, M, ldq, nullptr, h, C, ldc, stream);
+}
+
+tw_status tw_gemm_mx4_grouped(const void* Q, const void* S, int M, int ldq, const int32_t* offsets, tw_handle_t h, void* C,
+                              int ldc, void* stream) {
+  if (!offsets || ((uintptr_t)offsets & 3) || !h) return TW_ERR_ARG;
+  for (int32_t n : h->member_n)
+    if (n != h->member_n[0]) return TW_ERR_ARG;              // experts of one width
+  return gemm_mx4_launch(Q, S, M, ldq, offsets, h, C, ldc, stream);
 }
 
 tw_status tw_export(tw_handle_t h, tw_packed_view* out) {

@@ -93,7 +93,7 @@ constexpr int D8 = 3;        // stages in flight
 // KSPLIT = 2: two groups of four waves own the same output tile; a stage then holds 128
 // condensed rows, group g multiplies rows 64g..64g+63 of it and the partial sums are added
 // through LDS before the epilogue (long K with too few tiles to fill the chip).
-template <int TM, int TN, int WAVES_M, bool DENSE, bool OUT8, int NWAVES = 4, int KSPLIT = 1, bool VEC = false>
+template <int TM, int TN, int WAVES_M, bool DENSE, int OUT, int NWAVES = 4, int KSPLIT = 1, bool VEC = false>
 // (the 256 x 128 instance holds 128 accumulators per lane; its epilogue must not push the
 // register count past two waves per SIMD, which the 72 KiB of LDS allow)
 __global__ __launch_bounds__(NWAVES * 64, (TM * TN >= 256 * 128) ? 2 : 1) void tw_gemm_i8_kernel(GemmI8Args g) {
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(NWAVES * 64, (TM * TN >= 256 * 128) ? 2 : 1) void t
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_gemm = g.n_mtiles * g.n_tiles;
   if ((int)blockIdx.x >= n_gemm) {
-    zero_fill_column8<OUT8>(g, blockIdx.x - n_gemm);
+    zero_fill_column8<OUT>(g, blockIdx.x - n_gemm);
     return;
   }
   int mt, t;                             // t: launch position of the tile, then the tile itself
@@ -404,7 +404,63 @@ __global__ __launch_bounds__(NWAVES * 64, (TM * TN >= 256 * 128) ? 2 : 1) void t
     }
   }
 
-  if constexpr (OUT8) {
+  if constexpr (OUT == OUT_F16) {
+    // ---- epilogue, fp16 output with scales: stage the whole tile as halves [n][m] (rows of TM + 8), then one
+    // 16-byte streaming store of 8 m per thread; the tokens' scales lie behind the tile
+    constexpr int CS2 = TM * 2 + 16;
+    static_assert(TN * CS2 + TM * 4 <= LDS_BYTES, "");
+    constexpr int CA = TM / 8;                   // pieces per column
+    constexpr int RPP = NT / CA;                 // columns per pass
+    static_assert(TN % RPP == 0, "");
+    constexpr int NPASS = TN / RPP;
+    const int c = tid % CA, r0 = tid / CA;
+    const int m = m0 + c * 8;
+    int cols[NPASS];                             // original column of C of every piece (CTO_n)
+#pragma unroll
+    for (int i = 0; i < NPASS; ++i) cols[i] = g.col_idx[t * TN + r0 + i * RPP];
+    float ws[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int col = g.col_idx[t * TN + wn * WN + j * 32 + (lane & 31)];
+      ws[j] = col < 0 ? 0.f : g.w_scale[col];
+    }
+    __syncthreads();                             // the pipeline buffers are free
+    float* as = (float*)(lds + TN * CS2);
+    for (int i = tid; i < TM; i += NT) as[i] = g.a_scale[min(m0 + i, g.M - 1)];
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int mm = wm * WM + i * 32 + 8 * rq + 4 * (lane >> 5);
+        const floatx4 s4 = *(const floatx4*)(as + mm);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const int n = wn * WN + j * 32 + (lane & 31);
+          half4 v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = dequantize(acc[i][j][rq * 4 + r], s4[r], ws[j]);
+          *(half4*)(lds + n * CS2 + mm * 2) = v;
+        }
+      }
+    }
+    __syncthreads();
+    half8 pc[NPASS];
+#pragma unroll
+    for (int i = 0; i < NPASS; ++i) pc[i] = *(const half8*)(lds + (r0 + i * RPP) * CS2 + c * 16);
+#pragma unroll
+    for (int i = 0; i < NPASS; ++i) {
+      if (cols[i] < 0 || m >= g.M) continue;
+      _Float16* dst = (_Float16*)g.C + (size_t)cols[i] * g.ldc + m;
+      if (m + 8 <= g.M) __builtin_nontemporal_store(pc[i], (half8*)dst);
+      else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (m + e < g.M) dst[e] = pc[i][e];
+      }
+    }
+  } else if constexpr (OUT == OUT_I8) {
     // ---- epilogue, int8 output: requantise in registers, stage the whole tile as bytes
     // [n][m] (rows of TM + 16 bytes), then one 16-byte streaming store of 16 m per thread
     constexpr int CS8 = TM + 16;
@@ -534,10 +590,13 @@ static hipError_t launch8(const GemmI8Args& g, hipStream_t stream) {
   if (grid <= 0) return hipSuccess;
   auto go = [&](auto VEC_) {
     constexpr bool VEC = decltype(VEC_)::value;
-    if (g.c_i8)
-      return launch_kernel(tw_gemm_i8_kernel<TM, TN, WAVES_M, DENSE, true, NWAVES, KSPLIT, VEC>, dim3(grid), dim3(NWAVES * 64), stream, g);
+    if constexpr (!DENSE)
+      if (g.c_dtype == OUT_F16)
+        return launch_kernel(tw_gemm_i8_kernel<TM, TN, WAVES_M, DENSE, OUT_F16, NWAVES, KSPLIT, VEC>, dim3(grid), dim3(NWAVES * 64), stream, g);
+    if (g.c_dtype == OUT_I8)
+      return launch_kernel(tw_gemm_i8_kernel<TM, TN, WAVES_M, DENSE, OUT_I8, NWAVES, KSPLIT, VEC>, dim3(grid), dim3(NWAVES * 64), stream, g);
     else
-      return launch_kernel(tw_gemm_i8_kernel<TM, TN, WAVES_M, DENSE, false, NWAVES, KSPLIT, VEC>, dim3(grid), dim3(NWAVES * 64), stream, g);
+      return launch_kernel(tw_gemm_i8_kernel<TM, TN, WAVES_M, DENSE, OUT_I32, NWAVES, KSPLIT, VEC>, dim3(grid), dim3(NWAVES * 64), stream, g);
   };
   // Row indices by vector loads with at most two workgroups per CU (same buffers, scalar / vector, TW 75 %,
   // int8 output: 3072 x 768 at M = 4096 9.2 / 8.4 us, 768 x 768 5.5 / 5.3, 2048 x 2048 x 2048 of G = 64 at 80 %

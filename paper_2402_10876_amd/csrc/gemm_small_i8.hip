@@ -34,8 +34,8 @@ __device__ __forceinline__ int2v tr8_read(uint32_t addr) {
 
 }  // namespace
 
-// SP: 2:4 inside the kept rows (TVW).  NW: waves.  U: k-steps of a wave in flight.  OUT8: requantised output.
-template <bool SP, int NW, int U, bool OUT8>
+// SP: 2:4 inside the kept rows (TVW).  NW: waves.  U: k-steps of a wave in flight.  OUT: what is written (i8_common.h).
+template <bool SP, int NW, int U, int OUT>
 __global__ __launch_bounds__(NW * 64) void tw_gemm_small_i8_kernel(GemmI8Args g, int G, int n_blocks, int zero_cols_per_wg) {
   constexpr int NT = NW * 64;
   constexpr int KR = SP ? 64 : 32;                  // condensed rows per k-step
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(NW * 64) void tw_gemm_small_i8_kernel(GemmI8Args g,
   constexpr int PITCH = 36;                         // staged partial sums: [n][m] ints
   constexpr int AREA_A = U * NC * 1024, AREA_P = 32 * PITCH * 4;
   constexpr int AREA = ((AREA_A > AREA_P ? AREA_A : AREA_P) + 1023) / 1024 * 1024;   // LDS of one wave
-  constexpr int ES = OUT8 ? 1 : 4;
+  constexpr int ES = out_bytes<OUT>;
   __shared__ __attribute__((aligned(1024))) char lds[NW * AREA];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -213,7 +213,16 @@ __global__ __launch_bounds__(NW * 64) void tw_gemm_small_i8_kernel(GemmI8Args g,
       if (x >= (uint32_t)g.conv_W || y >= (uint32_t)g.conv_H) v[1] = 0;
     }
     const size_t to = (size_t)cols[i] * g.ldc + m;
-    if constexpr (OUT8) {
+    if constexpr (OUT == OUT_F16) {
+      const float w = g.w_scale[cols[i]];
+      const _Float16 lo = dequantize(v[0], g.a_scale[m], w), hi = dequantize(v[1], g.a_scale[min(m + 1, g.M - 1)], w);
+      if (m + 1 < g.M) {
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+        *(half2v*)((_Float16*)g.C + to) = half2v{lo, hi};
+      } else {
+        ((_Float16*)g.C)[to] = lo;
+      }
+    } else if constexpr (OUT == OUT_I8) {
       const int lo = requantize(v[0], g.scale), hi = requantize(v[1], g.scale);
       if (m + 1 < g.M) *(uint16_t*)((int8_t*)g.C + to) = (uint16_t)((lo & 0xff) | (hi & 0xff) << 8);
       else ((int8_t*)g.C)[to] = (int8_t)lo;
@@ -228,12 +237,14 @@ template <bool SP, int NW>
 static hipError_t launch_small8(int G, GemmI8Args& g, hipStream_t stream) {
   g.n_mtiles = (int)(((long)g.M + 31) / 32);
   const int n_blocks = g.n_tiles * (G / 32);
-  const int chunks = zero_chunks((int64_t)g.M * (g.c_i8 ? 1 : 4));
+  const int chunks = zero_chunks((int64_t)g.M * (g.c_dtype == OUT_I8 ? 1 : g.c_dtype == OUT_F16 ? 2 : 4));
   const int zper = chunks < NW * 64 ? NW * 64 / chunks : 1;       // pruned columns per workgroup that clears them
   const int grid = n_blocks * g.n_mtiles + (g.n_zero + zper - 1) / zper;
   if (grid <= 0) return hipSuccess;
-  if (g.c_i8) return launch_kernel(tw_gemm_small_i8_kernel<SP, NW, 4, true>, dim3(grid), dim3(NW * 64), stream, g, G, n_blocks, zper);
-  return launch_kernel(tw_gemm_small_i8_kernel<SP, NW, 4, false>, dim3(grid), dim3(NW * 64), stream, g, G, n_blocks, zper);
+  if (g.c_dtype == OUT_F16)
+    return launch_kernel(tw_gemm_small_i8_kernel<SP, NW, 4, OUT_F16>, dim3(grid), dim3(NW * 64), stream, g, G, n_blocks, zper);
+  if (g.c_dtype == OUT_I8) return launch_kernel(tw_gemm_small_i8_kernel<SP, NW, 4, OUT_I8>, dim3(grid), dim3(NW * 64), stream, g, G, n_blocks, zper);
+  return launch_kernel(tw_gemm_small_i8_kernel<SP, NW, 4, OUT_I32>, dim3(grid), dim3(NW * 64), stream, g, G, n_blocks, zper);
 }
 
 // Four waves hold 512 kept rows at once (TVW: 1024), eight twice that and one workgroup less per CU: 768 x 2304, M = 256 3.8 / 4.7 us with

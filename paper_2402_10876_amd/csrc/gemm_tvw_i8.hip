@@ -81,7 +81,7 @@ constexpr int KSV = 128;   // condensed rows per stage
 
 }  // namespace
 
-template <int TM, int TN, int WAVES_N, bool OUT8>
+template <int TM, int TN, int WAVES_N, int OUT>
 __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
   constexpr int NW = 4, NT = 256, D = 3;
   constexpr int WAVES_M = NW / WAVES_N;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_gemm = g.n_mtiles * g.n_tiles;
   if ((int)blockIdx.x >= n_gemm) {
-    zero_fill_column8<OUT8>(g, blockIdx.x - n_gemm);
+    zero_fill_column8<OUT>(g, blockIdx.x - n_gemm);
     return;
   }
   int mt, pos;
@@ -299,11 +299,11 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
 
   // ---- epilogue: acc[i][j][r] is C^T(n, m) with m = lane % 32 and
   // n = 8*(r/4) + 4*(lane/32) + r%4 inside the 32 x 32 block; staged as [n][m] (int32, or
-  // int8 requantised in registers), then every thread finishes (column, CH x m) pieces with
+  // int8 requantised or fp16 scaled in registers), then every thread finishes (column, CH x m) pieces with
   // one 16-byte streaming store each
-  constexpr int CH = OUT8 ? 16 : 4;
-  constexpr int ES = OUT8 ? 1 : 4;                        // bytes per staged element
-  constexpr int CSE = OUT8 ? TM + 16 : CS;                // staged row bytes
+  constexpr int ES = out_bytes<OUT>;                      // bytes per staged element
+  constexpr int CH = 16 / ES;
+  constexpr int CSE = OUT == OUT_I32 ? CS : TM * ES + 16; // staged row bytes
   constexpr int CA = TM / CH;
   constexpr int RPP = NT / CA;
   static_assert(TN % RPP == 0, "");
@@ -313,6 +313,18 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
   int cols[NPASS];
 #pragma unroll
   for (int i = 0; i < NPASS; ++i) cols[i] = g.col_idx[t * TN + r0 + i * RPP];
+  [[maybe_unused]] float as[MB];
+  [[maybe_unused]] float* ws = (float*)(lds + TN * CSE);   // fp16: the columns' scales behind the tile
+  if constexpr (OUT == OUT_F16) {
+    static_assert(TN * CSE + TN * 4 <= LDS_BYTES, "");
+#pragma unroll
+    for (int j = 0; j < MB; ++j) as[j] = g.a_scale[min(m0 + wm * WM + j * 32 + (lane & 31), g.M - 1)];
+    __syncthreads();
+    for (int i = tid; i < TN; i += NT) {
+      const int col = g.col_idx[t * TN + i];
+      ws[i] = col < 0 ? 0.f : g.w_scale[col];
+    }
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -322,7 +334,8 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int n = wn * WN + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-        if constexpr (OUT8) *(int8_t*)(lds + n * CSE + mm) = (int8_t)requantize(acc[i][j][r], g.scale);
+        if constexpr (OUT == OUT_F16) *(_Float16*)(lds + n * CSE + mm * 2) = dequantize(acc[i][j][r], as[j], ws[n]);
+        else if constexpr (OUT == OUT_I8) *(int8_t*)(lds + n * CSE + mm) = (int8_t)requantize(acc[i][j][r], g.scale);
         else *(int*)(lds + n * CSE + mm * 4) = acc[i][j][r];
       }
     }
@@ -330,10 +343,12 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
   int4v pc[NPASS];
 #pragma unroll
   for (int i = 0; i < NPASS; ++i) pc[i] = *(const int4v*)(lds + (r0 + i * RPP) * CSE + c * CH * ES);
-  if (g.conv_P) {                                // implicit img2col: padding lanes of the grid are 0
-    const int4v vm = (int4v)conv_valid_mask_i8<CH>(g, m);
+  if constexpr (OUT != OUT_F16) {
+    if (g.conv_P) {                              // implicit img2col: padding lanes of the grid are 0
+      const int4v vm = (int4v)conv_valid_mask_i8<CH>(g, m);
 #pragma unroll
-    for (int i = 0; i < NPASS; ++i) pc[i] &= vm;
+      for (int i = 0; i < NPASS; ++i) pc[i] &= vm;
+    }
   }
 #pragma unroll
   for (int i = 0; i < NPASS; ++i) {
@@ -344,7 +359,8 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
 #pragma unroll
       for (int e = 0; e < CH; ++e)
         if (m + e < g.M) {
-          if constexpr (OUT8) dst[e] = (char)(pc[i][e >> 2] >> (8 * (e & 3)));
+          if constexpr (OUT == OUT_F16) ((uint16_t*)dst)[e] = (uint16_t)(pc[i][e >> 1] >> (16 * (e & 1)));
+          else if constexpr (OUT == OUT_I8) dst[e] = (char)(pc[i][e >> 2] >> (8 * (e & 3)));
           else ((int*)dst)[e] = pc[i][e];
         }
     }
@@ -355,8 +371,9 @@ template <int TM, int TN, int WAVES_N>
 static hipError_t launch_tvw8(const GemmI8Args& g, hipStream_t stream) {
   const int grid = g.n_mtiles * g.n_tiles + g.n_zero;
   if (grid <= 0) return hipSuccess;
-  if (g.c_i8) return launch_kernel(tvw_gemm_i8_kernel<TM, TN, WAVES_N, true>, dim3(grid), dim3(256), stream, g);
-  return launch_kernel(tvw_gemm_i8_kernel<TM, TN, WAVES_N, false>, dim3(grid), dim3(256), stream, g);
+  if (g.c_dtype == OUT_F16) return launch_kernel(tvw_gemm_i8_kernel<TM, TN, WAVES_N, OUT_F16>, dim3(grid), dim3(256), stream, g);
+  if (g.c_dtype == OUT_I8) return launch_kernel(tvw_gemm_i8_kernel<TM, TN, WAVES_N, OUT_I8>, dim3(grid), dim3(256), stream, g);
+  return launch_kernel(tvw_gemm_i8_kernel<TM, TN, WAVES_N, OUT_I32>, dim3(grid), dim3(256), stream, g);
 }
 
 hipError_t launch_tvw_i8(int G, int tm, GemmI8Args g, hipStream_t stream) {

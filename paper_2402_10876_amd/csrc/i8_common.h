@@ -15,6 +15,20 @@ __device__ __forceinline__ int requantize(int sum, float scale) {
   return (int)x;
 }
 
+// What a product writes (c_dtype of the calls; 2: tw_gemm_i8_scaled).
+enum { OUT_I32 = 0, OUT_I8 = 1, OUT_F16 = 2 };
+template <int OUT>
+constexpr int out_bytes = OUT == OUT_I8 ? 1 : OUT == OUT_F16 ? 2 : 4;
+
+// int32 sum -> fp16: fp32(sum) and its product with the (fp32) product of the two scales, one rounding each.  (The empty
+// statement keeps the compiler from the mixed-precision instruction that rounds the product to fp16 at once, which
+// it takes in some of the kernels and not in others.)
+__device__ __forceinline__ _Float16 dequantize(int sum, float a_scale, float w_scale) {
+  float x = (float)sum * (a_scale * w_scale);
+  asm("" : "+v"(x));
+  return (_Float16)x;
+}
+
 // Implicit img2col: which of the CH wide-grid positions m .. m+CH-1 are output pixels (x < W and
 // y < H).  CH = 4: one all-ones dword per valid position (int32 output); CH = 16: one 0xff byte
 // per valid position (int8 output).  One division per thread.
@@ -35,10 +49,10 @@ __device__ __forceinline__ u32x4 conv_valid_mask_i8(const GemmI8Args& g, int m) 
 }
 
 // Extra workgroups of a launch write 0 into one pruned column of C each.
-template <bool OUT8>
+template <int OUT>
 __device__ __forceinline__ void zero_fill_column8(const GemmI8Args& g, int which) {
   const int col = g.zero_cols[which];
-  constexpr int ES = OUT8 ? 1 : 4;
+  constexpr int ES = out_bytes<OUT>;
   char* row = (char*)g.C + (size_t)col * g.ldc * ES;
   const size_t bytes = (size_t)g.M * ES;
   const u32x4 z = {0u, 0u, 0u, 0u};

@@ -48,10 +48,11 @@ struct GemmArgs {
 // Int8 operands, int32 sums (gemm_i8.hip); layouts as the KM kernels above.
 struct GemmI8Args {
   const int8_t* A;               // K x M bytes, element (i,k) at A[k*lda + i]
-  void* C;                       // N x M, int32 or (c_i8) requantised int8
+  void* C;                       // N x M, by c_dtype: 0 int32, 1 requantised int8, 2 fp16 with scales
   int M, lda, ldc;
-  int c_i8;
-  float scale;
+  int c_dtype;
+  float scale;                   // int8 output
+  const float *a_scale, *w_scale;// fp16 output: of the tokens (M) and of the columns (N)
   const int8_t* vals;            // TW: condensed image [sum Kp_t][G] bytes; dense: B, K x N row-major
   int ldb;                       // dense only
   const int32_t* row_idx;

@@ -12,6 +12,7 @@
 #include <new>
 
 #include "mk_band.h"
+#include "mx4_format.h"
 #include "packed.h"
 
 namespace twg {
@@ -219,6 +220,139 @@ tw_status pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* tile_
   return TW_ERR_ALLOC;
 }
 
+// Microscaled 4-bit weights: kept columns are those with any mask bit, cut into tiles of G; a tile keeps a block of 32 rows
+// whole if the mask keeps anything of it there.  `values` are what the blocks stand for (fp16).
+tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_s* h) try {
+  h->K = K; h->N = N; h->G = G; h->pattern = TW_PATTERN_TW; h->dtype = TW_DTYPE_MX4;
+  std::vector<int32_t> rows, offs;
+  structure_of(mask, K, N, G, h->col_idx, offs, rows);
+  const int n_tiles = (int)offs.size() - 1, KB = (K + MX4_BLOCK - 1) / MX4_BLOCK;
+  h->tile_k_off.assign(1, 0);
+  std::vector<uint8_t> kept(KB);
+  for (int t = 0; t < n_tiles; ++t) {          // whole blocks
+    std::fill(kept.begin(), kept.end(), 0);
+    for (int i = offs[t]; i < offs[t + 1]; ++i) kept[rows[i] / MX4_BLOCK] = 1;
+    for (int b = 0; b < KB; ++b)
+      if (kept[b])
+        for (int k = b * MX4_BLOCK; k < std::min(K, (b + 1) * MX4_BLOCK); ++k) h->row_idx.push_back(k);
+    h->tile_k_off.push_back((int32_t)h->row_idx.size());
+  }
+  set_tiles_of_G(h);
+  finish_lists(h);
+  uint16_t value[256][16];                     // fp16 bits of a code under a scale byte (those of finite blocks)
+  for (int s = MX4_ONE - 26; s <= MX4_ONE + 13; ++s)
+    for (int c = 0; c < 16; ++c) value[s][c] = mx4_value((uint8_t)c, (uint8_t)s);
+  h->values.resize((size_t)h->sum_kw);
+  uint16_t top[128];
+  uint8_t scale[128];
+  for (int t = 0; t < n_tiles; ++t) {
+    const int w = h->tile_col_off[t + 1] - h->tile_col_off[t];
+    const int32_t* cols = h->col_idx.data() + h->tile_col_off[t];
+    uint16_t* v = h->values.data() + h->val_off[t];
+    for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1];) {
+      const int k0 = h->row_idx[i], n = std::min(K - k0, MX4_BLOCK);
+      std::fill(top, top + w, (uint16_t)0);
+      for (int k = 0; k < n; ++k) {
+        const size_t row = (size_t)(k0 + k) * N;
+        for (int c = 0; c < w; ++c) {
+          const uint16_t x = mask[row + cols[c]] ? B[row + cols[c]] : (uint16_t)0;
+          v[(size_t)k * w + c] = x;
+          top[c] = std::max(top[c], (uint16_t)(x & 0x7fff));
+        }
+      }
+      for (int c = 0; c < w; ++c) {
+        if (top[c] >= 0x7c00) return TW_ERR_ARG;
+        scale[c] = mx4_scale_of(top[c]);
+      }
+      for (int k = 0; k < n; ++k)
+        for (int c = 0; c < w; ++c) {
+          uint16_t& x = v[(size_t)k * w + c];
+          x = value[scale[c]][mx4_code(x, scale[c])];
+        }
+      v += (size_t)n * w;
+      i += n;
+    }
+  }
+  build_device_image(h);
+  return TW_OK;
+} catch (const std::bad_alloc&) {
+  return TW_ERR_ALLOC;
+}
+
+// The image of a microscaled 4-bit weight from its logical form (layout at Mx4Image).
+static void build_mx4_image(tw_handle_s* h) {
+  Mx4Image& d = h->mx4;
+  const int G = h->G, GB = G / 32;
+  std::vector<int32_t> members = h->member_n;
+  if (members.empty()) members.assign(1, h->N);
+  d.member_tile.assign(1, 0); d.member_col.assign(1, 0);
+  std::vector<uint8_t> is_kept(h->N, 0);
+  for (int32_t c : h->col_idx) is_kept[c] = 1;
+  int64_t step = 0;
+  int t = 0;
+  for (int32_t n : members) {                  // tiles
+    const int first = (int)d.tiles.size(), col1 = d.member_col.back() + n;
+    const int z0 = (int)d.zero_cols.size();
+    for (int c = d.member_col.back(); c < col1; ++c)
+      if (!is_kept[c]) d.zero_cols.push_back(c);
+    const int zeros = (int)d.zero_cols.size() - z0;
+    for (; t < h->n_tiles && h->col_idx[h->tile_col_off[t]] < col1; ++t) {
+      Mx4Tile r{};
+      r.step0 = step;
+      for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1]; ++i)
+        if (h->row_idx[i] % MX4_BLOCK == 0) d.blocks.push_back((uint16_t)(h->row_idx[i] / MX4_BLOCK));
+      if (d.blocks.size() % 2) d.blocks.push_back(d.blocks.back());
+      step = (int64_t)d.blocks.size() / 2;
+      r.steps = (int32_t)(step - r.step0);
+      d.tiles.push_back(r);
+      for (int j = 0; j < G; ++j) {
+        const int c = h->tile_col_off[t] + j;
+        d.col_idx.push_back(c < h->tile_col_off[t + 1] ? h->col_idx[c] : -1);
+      }
+    }
+    if ((int)d.tiles.size() == first) {
+      Mx4Tile r{};
+      r.step0 = step;
+      d.tiles.push_back(r);
+      d.col_idx.insert(d.col_idx.end(), G, -1);
+    }
+    const int tiles = (int)d.tiles.size() - first;
+    for (int i = 0; i < tiles; ++i) {
+      d.tiles[first + i].zero_beg = z0 + (int)((int64_t)zeros * i / tiles);
+      d.tiles[first + i].zero_end = z0 + (int)((int64_t)zeros * (i + 1) / tiles);
+    }
+    d.max_member_tiles = std::max(d.max_member_tiles, tiles);
+    d.member_tile.push_back((int32_t)d.tiles.size());
+    d.member_col.push_back(col1);
+  }
+  d.vals.assign((size_t)step * GB * 1024, 0);
+  d.scales.assign((size_t)step * GB * 64, (uint8_t)MX4_ONE);
+  int64_t s0 = 0;
+  uint16_t top[128];
+  for (int tl = 0; tl < h->n_tiles; ++tl) {    // values (the tiles that keep nothing have no steps)
+    const int w = h->tile_col_off[tl + 1] - h->tile_col_off[tl];
+    const uint16_t* v = h->values.data() + h->val_off[tl];
+    int b = 0;
+    for (int i = h->tile_k_off[tl]; i < h->tile_k_off[tl + 1]; ++b) {
+      const int n = std::min(h->K - h->row_idx[i], MX4_BLOCK);
+      const int64_t s = s0 + b / 2;
+      std::fill(top, top + w, (uint16_t)0);
+      for (int k = 0; k < n; ++k)
+        for (int c = 0; c < w; ++c) top[c] = std::max(top[c], (uint16_t)(v[(size_t)k * w + c] & 0x7fff));
+      for (int c = 0; c < w; ++c) {
+        const int lane = c % 32 + 32 * (b % 2), nb = c / 32;
+        const uint8_t sc = mx4_scale_of(top[c]);
+        d.scales[((size_t)s * 64 + lane) * GB + nb] = sc;
+        uint8_t* out = d.vals.data() + (((size_t)s * GB + nb) * 64 + lane) * 16;
+        for (int k = 0; k < n; ++k) out[k / 2] |= (uint8_t)(mx4_code(v[(size_t)k * w + c], sc) << (4 * (k % 2)));
+      }
+      v += (size_t)n * w;
+      i += n;
+    }
+    s0 += (b + 1) / 2;
+  }
+}
+
 tw_status unpack_host(const tw_handle_s* h, uint16_t* Bm, uint8_t* mask) {
   const size_t total = (size_t)h->K * h->N;
   if (Bm) std::memset(Bm, 0, total * sizeof(uint16_t));
@@ -291,6 +425,7 @@ tw_status concat_host(const tw_handle_s* const* parts, int n, tw_handle_s* h) tr
       h->ew_row.insert(h->ew_row.end(), p->ew_row.begin(), p->ew_row.end());
       h->ew_val.insert(h->ew_val.end(), p->ew_val.begin(), p->ew_val.end());
     }
+    h->member_n.push_back(p->N);
     h->N += p->N; h->n_kept += p->n_kept; h->n_tiles += p->n_tiles;
     h->sum_kw += p->sum_kw; h->sum_k += p->sum_k; h->nonfinite |= p->nonfinite;
   }
@@ -327,6 +462,7 @@ tw_status concat_host(const tw_handle_s* const* parts, int n, tw_handle_s* h) tr
 //      16-bit half selected by its ABID field, 2 bits per stored element).
 // ---------------------------------------------------------------------------
 void build_device_image(tw_handle_s* h) {
+  if (h->dtype == TW_DTYPE_MX4) { build_mx4_image(h); return; }
   build_device_lists(h);
   build_device_values(h);
 }

@@ -67,6 +67,27 @@ enum { IMG_TILE_KP_OFF, IMG_TILE_ORDER, IMG_TILE_SCHED, IMG_COL_IDX, IMG_ROW_IDX
        IMG_EW_PTR, IMG_EW_PAIRS, IMG_VALID, IMG_PARTS };
 struct ImageLayout { size_t bytes[IMG_PARTS], off[IMG_PARTS], total; };
 
+// Device image of a microscaled 4-bit weight (dtype TW_DTYPE_MX4).  A tile's kept blocks of 32 rows go two by two through
+// v_mfma_scale_f32_32x32x64_f8f6f4: a step is two blocks (the second one zeros where the number is odd).
+struct Mx4Tile {               // one record per tile, read by a workgroup as it starts
+  int64_t step0;               // first step: of `blocks` (two each), `vals` and `scales`
+  int32_t steps;
+  int32_t zero_beg, zero_end;  // pruned columns that the tile's workgroups clear (zero_cols)
+  int32_t pad[3];
+};
+struct Mx4Image {
+  std::vector<Mx4Tile> tiles;          // per member its tiles, at least one (a member that keeps nothing has a tile of no steps)
+  std::vector<int32_t> member_tile;    // n_members + 1: tiles of a member
+  std::vector<int32_t> member_col;     // n_members + 1: columns of a member
+  std::vector<uint16_t> blocks;        // 2 per step: number of the block (a repeated one where the number is odd)
+  std::vector<int32_t> col_idx;        // G per tile: original column, -1 = none
+  std::vector<int32_t> zero_cols;
+  std::vector<uint8_t> vals;           // per step and column block of 32: [lane][16 bytes], lane l = column l % 32, block l / 32
+  std::vector<uint8_t> scales;         // per step: [lane][G / 32 bytes], byte j: column block j
+  int32_t max_member_tiles = 0;
+  size_t off[7] = {}, off_scales = 0;  // of the parts above in the device allocation, in this order; of `scales`
+};
+
 }  // namespace twg
 
 struct tw_handle_s {
@@ -83,7 +104,9 @@ struct tw_handle_s {
   int32_t k_union = 0;  // K rows kept by at least one tile
   int32_t max_kp = 0;  // largest padded K_t
   bool nonfinite = false;  // fp16 TW with K > MK_KC: an infinity or NaN among the values
+  std::vector<int32_t> member_n;     // columns of the parts that tw_concat joined (empty: not joined)
   twg::DeviceImage img;
+  twg::Mx4Image mx4;                 // dtype TW_DTYPE_MX4 only; the allocation is img.blob
   // device-side packing (tw_pack_dev): the lists and the values live in the device image alone until
   // somebody asks for them on the host
   bool host_lists_ready = true, host_values_ready = true;
@@ -94,6 +117,9 @@ namespace twg {
 tw_status pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* tile_mask,
                     int K, int N, int G, int pattern, tw_handle_s* h);
 tw_status unpack_host(const tw_handle_s* h, uint16_t* Bm, uint8_t* mask);
+// The same for a microscaled 4-bit weight: any mask; the logical form is that of a TW weight whose tiles keep whole blocks
+// of 32 rows, with the values that the blocks stand for.  TW_ERR_ARG for a kept weight that is not finite.
+tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_s* h);
 // Fills *h with parts[0..n) side by side along N (same K, G and pattern).
 tw_status concat_host(const tw_handle_s* const* parts, int n, tw_handle_s* h);
 // Launch order of the tiles, read when a device image is built: 1 = longest K_t first.
