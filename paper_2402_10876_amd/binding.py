@@ -36,7 +36,7 @@ class _Unbound:
     def gemm(*_):
         return None
 
-    gemm_i8 = conv = conv_i8 = gemm
+    gemm_i8 = conv = conv_i8 = rmsnorm = quant_i8 = gemm_i8_scaled = quant_mx4 = gemm_mx4 = gemm_mx4_grouped = gemm
 
 
 _call = _Unbound     # the launch calls as a CPython module; None for arguments that ctypes has to convert
@@ -50,7 +50,9 @@ def _bind_call(L):
     loader = importlib.machinery.ExtensionFileLoader("_twcall", p)
     m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_twcall", p, loader=loader))
     loader.exec_module(m)
-    m.bind(*(C.cast(f, C.c_void_p).value for f in (L.tw_gemm, L.tw_gemm_i8, L.tw_conv_gemm, L.tw_conv_gemm_i8)))
+    m.bind(*(C.cast(f, C.c_void_p).value for f in (
+        L.tw_gemm, L.tw_gemm_i8, L.tw_conv_gemm, L.tw_conv_gemm_i8, L.tw_rmsnorm, L.tw_quant_i8, L.tw_gemm_i8_scaled, L.tw_quant_mx4,
+        L.tw_gemm_mx4, L.tw_gemm_mx4_grouped)))
     _call = m
 
 
@@ -392,34 +394,58 @@ def tw_rmsnorm(X_ptr: int, R_ptr, gamma_ptr, eps: float, M: int, K: int, ld: int
                stream: int = 0):
     """Residual sum, root-mean-square norm, output in int8 with a scale per token and / or in fp16; addresses that may be
     None: R, gamma, H, Y, and Q with scale (see include/twgemm.h)."""
-    _check(lib().tw_rmsnorm(X_ptr, R_ptr, gamma_ptr, eps, M, K, ld, H_ptr, Y_ptr, Q_ptr, ldq, scale_ptr, stream), "tw_rmsnorm")
+    st = _call.rmsnorm(X_ptr, R_ptr, gamma_ptr, eps, M, K, ld, H_ptr, Y_ptr, Q_ptr, ldq, scale_ptr, stream)
+    if st is None:
+        st = lib().tw_rmsnorm(X_ptr, R_ptr, gamma_ptr, eps, M, K, ld, H_ptr, Y_ptr, Q_ptr, ldq, scale_ptr, stream)
+    if st:
+        raise TwError(st, "tw_rmsnorm")
 
 
 def tw_quant_i8(X_ptr: int, M: int, K: int, ldx: int, Q_ptr: int, ldq: int, scale_ptr: int, stream: int = 0):
     """fp16 activations (K x M) to int8 with a scale per token."""
-    _check(lib().tw_quant_i8(X_ptr, M, K, ldx, Q_ptr, ldq, scale_ptr, stream), "tw_quant_i8")
+    st = _call.quant_i8(X_ptr, M, K, ldx, Q_ptr, ldq, scale_ptr, stream)
+    if st is None:
+        st = lib().tw_quant_i8(X_ptr, M, K, ldx, Q_ptr, ldq, scale_ptr, stream)
+    if st:
+        raise TwError(st, "tw_quant_i8")
 
 
 def tw_gemm_i8_scaled(A_ptr: int, M: int, lda: int, packed: PackedWeight, a_scale_ptr: int, w_scale_ptr: int, C_ptr: int,
                       ldc: int, stream: int = 0):
     """int8 A times a packed int8 weight; C (N x M) fp16 = sums * a_scale (of the token) * w_scale (of the column)."""
-    _check(lib().tw_gemm_i8_scaled(A_ptr, M, lda, packed.handle, a_scale_ptr, w_scale_ptr, C_ptr, ldc, stream), "tw_gemm_i8_scaled")
+    st = _call.gemm_i8_scaled(A_ptr, M, lda, packed._addr, a_scale_ptr, w_scale_ptr, C_ptr, ldc, stream)
+    if st is None:
+        st = lib().tw_gemm_i8_scaled(A_ptr, M, lda, packed.handle, a_scale_ptr, w_scale_ptr, C_ptr, ldc, stream)
+    if st:
+        raise TwError(st, "tw_gemm_i8_scaled")
 
 
 def tw_quant_mx4(X_ptr: int, M: int, K: int, ldx: int, layout: int, Q_ptr: int, S_ptr: int, ldq: int, stream: int = 0):
     """fp16 activations to microscaled 4-bit blocks: codes (ceil(K/32) x ldq x 16 bytes) and scale bytes (ceil(K/32) x ldq)."""
-    _check(lib().tw_quant_mx4(X_ptr, M, K, ldx, layout, Q_ptr, S_ptr, ldq, stream), "tw_quant_mx4")
+    st = _call.quant_mx4(X_ptr, M, K, ldx, layout, Q_ptr, S_ptr, ldq, stream)
+    if st is None:
+        st = lib().tw_quant_mx4(X_ptr, M, K, ldx, layout, Q_ptr, S_ptr, ldq, stream)
+    if st:
+        raise TwError(st, "tw_quant_mx4")
 
 
 def tw_gemm_mx4(Q_ptr: int, S_ptr: int, M: int, ldq: int, packed: PackedWeight, C_ptr: int, ldc: int, stream: int = 0):
     """4-bit activations times a 4-bit weight; C (N x M) fp16."""
-    _check(lib().tw_gemm_mx4(Q_ptr, S_ptr, M, ldq, packed.handle, C_ptr, ldc, stream), "tw_gemm_mx4")
+    st = _call.gemm_mx4(Q_ptr, S_ptr, M, ldq, packed._addr, C_ptr, ldc, stream)
+    if st is None:
+        st = lib().tw_gemm_mx4(Q_ptr, S_ptr, M, ldq, packed.handle, C_ptr, ldc, stream)
+    if st:
+        raise TwError(st, "tw_gemm_mx4")
 
 
 def tw_gemm_mx4_grouped(Q_ptr: int, S_ptr: int, M: int, ldq: int, offsets_ptr: int, packed: PackedWeight, C_ptr: int, ldc: int,
                         stream: int = 0):
     """The same by expert: tokens offsets[e] .. offsets[e+1]-1 (int32 on the device) meet member e of a tw_concat handle."""
-    _check(lib().tw_gemm_mx4_grouped(Q_ptr, S_ptr, M, ldq, offsets_ptr, packed.handle, C_ptr, ldc, stream), "tw_gemm_mx4_grouped")
+    st = _call.gemm_mx4_grouped(Q_ptr, S_ptr, M, ldq, offsets_ptr, packed._addr, C_ptr, ldc, stream)
+    if st is None:
+        st = lib().tw_gemm_mx4_grouped(Q_ptr, S_ptr, M, ldq, offsets_ptr, packed.handle, C_ptr, ldc, stream)
+    if st:
+        raise TwError(st, "tw_gemm_mx4_grouped")
 
 
 class ConvBinding:

@@ -5,7 +5,7 @@
 //   y = fp16(g * inv);  scale = max |g| * inv / 127;  q = nearest integer of 127 g / max |g|, ties to even
 //
 // inv cancels in q, which is therefore exact: u = fma(g, fl(127 / max|g|), 1.5 * 2^23) rounds to an integer in the low byte of
-// u, wrong only within 127 * 2^-24 of a half; where the distance to n is more than 0.4999 the side is settled in 64 bits
+// u, wrong only within 127 * 2^-24 of a half; where the distance to n is more than 0.49998 the side is settled in 64 bits
 // (254 g against (2n +- 1) max|g|, both exact).  Sums of squares are fp32 (at most 32 terms a lane, then a tree).
 //
 // Bound by memory: 2 bytes in per value (4 with a residual), 1 to 5 out.  One workgroup owns 32 tokens and all K rows and
@@ -19,9 +19,8 @@ namespace twg {
 
 namespace {
 
-constexpr int TOK = 32;                  // tokens of a workgroup: 64 bytes of every row
-constexpr int LPR = TOK / 8;             // lanes per row, 8 tokens each
 constexpr float MAGIC = 12582912.f;      // 1.5 * 2^23
+constexpr uint32_t INF_BITS = 0x7f800000u;
 
 // The integer nearest to 127 g / top where n is next to a half away (d: which side).
 __device__ __forceinline__ float settle(float g, float top, float n, float d) {
@@ -32,92 +31,202 @@ __device__ __forceinline__ float settle(float g, float top, float n, float d) {
   return (x < edge || (x == edge && odd)) ? n - 1.f : n;
 }
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
+}
+
+// Workgroup -> its first token.  The workgroups of a line of memory (64 tokens) run on one XCD, whose L2 then fetches it once.
+// An XCD owns every other line of a quarter of the row: with all lines of an eighth, rows of a power of two of bytes meet half
+// of its L2's channels or fewer.
+constexpr int lines_of(int64_t M) { return (int)((M + 63) / 64); }
+template <int TOK>
+__device__ __forceinline__ int first_token(int bid, int n_wg) {
+  constexpr int WPL = 64 / TOK;
+  const int xcd = bid & 7, slot = bid >> 3, per = n_wg / (8 * WPL);
+  const int line = (xcd >> 1) * 2 * per + slot / WPL * 2 + (xcd & 1);
+  return line * 64 + slot % WPL * TOK;
+}
+
+// Eight values of a lane over the four rows of 16 lanes: x[0], x[1] of row r become the results for values 2 (r % 2) +
+// 4 (r / 2) and the next.
+template <class F>
+__device__ __forceinline__ void halve(float (&x)[8], F f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e + 4]), false, false);
+    x[e] = f(__uint_as_float(v[0]), __uint_as_float(v[1]));
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e + 2]), false, false);
+    x[e] = f(__uint_as_float(v[0]), __uint_as_float(v[1]));
+  }
+}
+// Over the lanes of a row of 16 that are LPR apart.
+template <int LPR, class F>
+__device__ __forceinline__ float around(float x, F f) {
+  auto turn = [&](auto N) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + decltype(N)::value, 0xf, 0xf, true));
+  };
+  x = f(x, turn(std::integral_constant<int, 8>{}));
+  if constexpr (LPR < 8) x = f(x, turn(std::integral_constant<int, 4>{}));
+  if constexpr (LPR < 4) x = f(x, turn(std::integral_constant<int, 2>{}));
+  if constexpr (LPR < 2) x = f(x, turn(std::integral_constant<int, 1>{}));
+  return x;
+}
+
 }  // namespace
 
-// NT threads; NCH: rows a lane keeps (0: more than fit, the second pass reads them again).
-template <bool NORM, int NT, int NCH>
+// TOK tokens and NT threads per workgroup; a lane keeps NCH rows in registers and NL in LDS (NCH = 0: more than fit, the
+// second pass reads them again).
+template <bool NORM, int TOK, int NT, int NCH, int NL = 0>
 __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
+  constexpr int LPR = TOK / 8;           // lanes per row, 8 tokens each
   constexpr int RPP = NT / LPR;          // rows per pass
   constexpr int NW = NT / 64;
-  __shared__ float s_sum[NW][TOK];
-  __shared__ uint32_t s_top[NW][TOK];
-  __shared__ float s_inv[TOK], s_mul[TOK], s_max[TOK];
+  __shared__ half8 s_h[NL ? NL : 1][NL ? NT : 1];
+  __shared__ __attribute__((aligned(16))) float s_sum[NW][TOK];
+  __shared__ __attribute__((aligned(16))) uint32_t s_top[NW][TOK];
+  __shared__ __attribute__((aligned(16))) float s_inv[TOK], s_mul[TOK], s_max[TOK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int m0 = xcd_remap(blockIdx.x, gridDim.x) * TOK;
+  const int m0 = first_token<TOK>(blockIdx.x, gridDim.x);
+  if (m0 >= g.M) return;
   const int c = tid % LPR, r0 = tid / LPR;
   const int m = m0 + c * 8;
   const bool live = m < g.M;
-  const size_t at = live ? (size_t)m : (size_t)m0;
+  const uint64_t lane_at = ((uint64_t)r0 * g.ld + (live ? c * 8 : 0)) * 2;   // bytes from row i * RPP, token m0
   const bool whole = m + 8 <= g.M;
+  const int tail = g.M & 7;              // tokens of the one piece that is not
   const int n_ch = (g.K + RPP - 1) / RPP;
 
-  auto load_h = [&](int i) {             // rows behind K: zeros
-    const int k = r0 + i * RPP, kc = min(k, g.K - 1);
-    half8 x = *(const half8*)(g.X + (size_t)kc * g.ld + at);
-    if (NORM && g.R) x += *(const half8*)(g.R + (size_t)kc * g.ld + at);
-    if (k >= g.K) x = half8{0, 0, 0, 0, 0, 0, 0, 0};
-    return x;
+  // Rows r0 + (i0 + i) * RPP, i < N: values (rows behind K: zeros) and gammas.  Every kind of load or store is a loop of its
+  // own behind one uniform branch, so that all of a kind are under way at once.
+  auto load_x = [&](const _Float16* from, int i) {      // (lanes behind K: a row in front of it)
+    const int k = i * RPP;
+    const char* row = (const char*)(from + (size_t)(k < g.K ? k : 0) * g.ld + m0);
+    return *(const half8*)(row + (r0 + k < g.K ? lane_at : 0));
   };
-  auto gamma_of = [&](int i) -> float {
-    if constexpr (!NORM) return 1.f;
-    return g.gamma ? (float)g.gamma[min(r0 + i * RPP, g.K - 1)] : 1.f;
+  auto load_h = [&](int i0, auto& h) {
+    constexpr int N = sizeof(h) / sizeof(half8), B = N < 8 ? N : N == 8 ? 8 : 4;
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = load_x(g.X, i0 + i);
+    if (NORM && g.R) {
+#pragma unroll
+      for (int b = 0; b < N; b += B) {
+        half8 r[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) r[i] = load_x(g.R, i0 + b + i);
+#pragma unroll
+        for (int i = 0; i < B; ++i) h[b + i] += r[i];
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (r0 + (i0 + i) * RPP >= g.K) h[i] = half8{0, 0, 0, 0, 0, 0, 0, 0};
+  };
+  auto load_gamma = [&](int i0, auto& gam) {
+    constexpr int N = sizeof(gam) / sizeof(_Float16);
+#pragma unroll
+    for (int i = 0; i < N; ++i) gam[i] = (_Float16)1.f;
+    if (NORM && g.gamma) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) gam[i] = g.gamma[min(r0 + (i0 + i) * RPP, g.K - 1)];
+    }
   };
   auto store_half = [&](_Float16* to, int i, half8 v) {
     const int k = r0 + i * RPP;
     if (k >= g.K || !live) return;
-    _Float16* p = to + (size_t)k * g.ld + m;
+    _Float16* p = (_Float16*)((char*)(to + (size_t)(i * RPP) * g.ld + m0) + lane_at);
     if (whole) *(half8*)p = v;
     else
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (m + e < g.M) p[e] = v[e];
+      for (int e = 0; e < 7; ++e)
+        if (e < tail) p[e] = v[e];
   };
 
-  float sum[8];
-  uint32_t top[8];
+  // Norm: sums of squares and the largest |g|, as fp32; an infinity or NaN among the h of a token shows in its sum, one
+  // among the gamma makes every token one that is not finite.  Quantiser: the largest magnitude over the fp16 bits.
+  float sum[NORM ? 8 : 1], top[NORM ? 8 : 1], worst = 0.f;
+  uint32_t bits[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) { sum[e] = 0.f; top[e] = 0u; }
+  for (int e = 0; e < (NORM ? 8 : 1); ++e) { sum[e] = 0.f; top[e] = 0.f; }
   auto stats = [&](half8 h, float gam) {
+    if constexpr (NORM) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = (float)h[e];
+        sum[e] = __builtin_fmaf(f, f, sum[e]);
+        top[e] = __builtin_fmaxf(top[e], __builtin_fabsf(f * gam));
+      }
+      worst = __builtin_fmaf(gam, 0.f, worst);         // NaN once a gamma is not finite
+    } else {
+      const u32x4 v = __builtin_bit_cast(u32x4, h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bits[e] = max_u16x2(bits[e], v[e] & 0x7fff7fffu);
+    }
+  };
+
+  constexpr int NG = NCH ? NCH : 4;      // rows of a lane that are held at a time
+  half8 h[NG];
+  _Float16 gam[NG];
+  auto first_pass = [&](int i0) {
+    load_gamma(i0, gam);
+    load_h(i0, h);
+    if (NORM && g.H) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) store_half(g.H, i0 + i, h[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NG; ++i) stats(h[i], (float)gam[i]);
+  };
+  if constexpr (NL > 0) {
+    static_assert(NL <= NCH, "");
+    first_pass(NCH);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) s_h[i][tid] = h[i];
+  }
+  if constexpr (NCH > 0) first_pass(0);
+  else
+    for (int i0 = 0; i0 < n_ch; i0 += NG) first_pass(i0);
+
+  // Over the lanes with the same tokens: two swaps between rows of 16 lanes halve the values of a lane (row r keeps tokens
+  // 2 (r % 2) + 4 (r / 2) and the next one of its piece), then rotations inside the row; no LDS instruction (with
+  // shuffles, 102 a wave, one token of 4096 values took 9 us, with these 5.6).
+  const int tok = c * 8 + 2 * (lane >> 4 & 1) + 4 * (lane >> 5);
+  if constexpr (NORM) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += worst;
+    halve(sum, [](float x, float y) { return x + y; });
+    halve(top, [](float x, float y) { return __builtin_fmaxf(x, y); });
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      sum[e] = around<LPR>(sum[e], [](float x, float y) { return x + y; });
+      top[e] = around<LPR>(top[e], [](float x, float y) { return __builtin_fmaxf(x, y); });
+    }
+    if ((lane & 15) < LPR)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        s_sum[wave][tok + e] = sum[e];
+        s_top[wave][tok + e] = sum[e] < __builtin_inff() ? __float_as_uint(top[e]) : INF_BITS;
+      }
+  } else {
+    float t8[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float f = (float)h[e];
-      if constexpr (NORM) sum[e] = __builtin_fmaf(f, f, sum[e]);
-      top[e] = max(top[e], __float_as_uint(f * gam) & 0x7fffffffu);      // (NaN above infinity above the numbers)
+      const uint32_t b = bits[e >> 1] >> (16 * (e & 1)) & 0xffffu;
+      t8[e] = __uint_as_float(b);        // (ordered as floats of 2^-126 and less: the comparison below is one of integers)
     }
-  };
-
-  half8 keep[NCH ? NCH : 1];
-  float gam[NCH ? NCH : 1];
-  if constexpr (NCH > 0) {
+    auto most = [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); };
+    halve(t8, most);
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) { keep[i] = load_h(i); gam[i] = gamma_of(i); }
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      if (NORM && g.H) store_half(g.H, i, keep[i]);
-      stats(keep[i], gam[i]);
-    }
-  } else {
-    for (int i = 0; i < n_ch; ++i) {
-      const half8 h = load_h(i);
-      if (NORM && g.H) store_half(g.H, i, h);
-      stats(h, gamma_of(i));
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t b = __float_as_uint(around<LPR>(t8[e], most));
+      if ((lane & 15) < LPR)
+        s_top[wave][tok + e] = b >= 0x7c00u ? INF_BITS : __float_as_uint((float)__builtin_bit_cast(_Float16, (unsigned short)b));
     }
   }
-
-  // sums and maxima over the lanes with the same tokens, then over the waves
-#pragma unroll
-  for (int d = LPR; d < 64; d *= 2)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (NORM) sum[e] += __shfl_xor(sum[e], d);
-      top[e] = max(top[e], (uint32_t)__shfl_xor((int)top[e], d));
-    }
-  if (lane < LPR)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (NORM) s_sum[wave][lane * 8 + e] = sum[e];
-      s_top[wave][lane * 8 + e] = top[e];
-    }
   __syncthreads();
   if (tid < TOK) {
     float s = 0.f;
@@ -129,7 +238,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
     }
     float inv = 1.f;
     if constexpr (NORM) inv = 1.f / sqrtf(s / (float)g.K + g.eps);
-    const bool fine = t != 0 && t < 0x7f800000u;
+    const bool fine = t != 0 && t < INF_BITS;
     const float big = __uint_as_float(t);
     s_inv[tid] = inv;
     s_max[tid] = big;
@@ -142,77 +251,114 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) { inv[e] = s_inv[c * 8 + e]; mul[e] = s_mul[c * 8 + e]; }
 
-  auto finish = [&](int i, half8 h, float gm) {
-    float f[8];
+  auto store_y = [&](int i, half8 x, float gm) {
+    half8 y;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = (float)h[e] * gm;
-    if (NORM && g.Y) {
-      half8 y;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = (_Float16)(f[e] * inv[e]);
-      store_half(g.Y, i, y);
-    }
-    if (!g.Q) return;
-    float u[8], d[8], far = 0.f;
+    for (int e = 0; e < 8; ++e) y[e] = (_Float16)((float)x[e] * gm * inv[e]);
+    store_half(g.Y, i, y);
+  };
+  auto store_q = [&](int i, half8 x, float gm) {
+    float f[8], u[8], d[8], far = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      f[e] = NORM ? (float)x[e] * gm : (float)x[e];
       u[e] = __builtin_fmaf(f[e], mul[e], MAGIC);
-      d[e] = __builtin_fmaf(f[e], mul[e], -(u[e] - MAGIC));
+      d[e] = __builtin_fmaf(f[e], mul[e], MAGIC - u[e]);
       far = __builtin_fmaxf(far, __builtin_fabsf(d[e]));
     }
-    if (far > 0.4999f) {
+    if (far > 0.49998f) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (__builtin_fabsf(d[e]) > 0.4999f) u[e] = settle(f[e], s_max[c * 8 + e], u[e] - MAGIC, d[e]) + MAGIC;
+        if (__builtin_fabsf(d[e]) > 0.49998f) u[e] = settle(f[e], s_max[c * 8 + e], u[e] - MAGIC, d[e]) + MAGIC;
     }
-    uint32_t q[2] = {0u, 0u};
+    uint32_t q[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e >> 2] |= (__float_as_uint(u[e]) & 0xffu) << (8 * (e & 3));
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 1]), __float_as_uint(u[4 * e]), 0x0c0c0400u);
+      const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 3]), __float_as_uint(u[4 * e + 2]), 0x04000c0cu);
+      q[e] = lo | hi;
+    }
     const int k = r0 + i * RPP;
     if (k >= g.K || !live) return;
-    int8_t* p = g.Q + (size_t)k * g.ldq + m;
+    int8_t* p = g.Q + (size_t)(i * RPP) * g.ldq + m0 + ((uint64_t)r0 * g.ldq + c * 8);
     if (whole) *(uint2*)p = make_uint2(q[0], q[1]);
     else
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (m + e < g.M) p[e] = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
+      for (int e = 0; e < 7; ++e)
+        if (e < tail) p[e] = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
+  };
+  auto second_pass = [&](int i0) {
+    if (NORM && g.Y) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) store_y(i0 + i, h[i], (float)gam[i]);
+    }
+    if (g.Q) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) store_q(i0 + i, h[i], (float)gam[i]);
+    }
   };
   if constexpr (NCH > 0) {
+    if constexpr (NCH > 8) load_gamma(0, gam);
+    second_pass(0);
+    if constexpr (NL > 0) {
+      load_gamma(NCH, gam);
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) finish(i, keep[i], gam[i]);
-  } else {
-    for (int i = 0; i < n_ch; ++i) {
-      half8 h;
-      if (NORM && g.H) {                 // (this lane's own stores; X or R may be the same buffer)
-        const int k = r0 + i * RPP, kc = min(k, g.K - 1);
-        h = half8{0, 0, 0, 0, 0, 0, 0, 0};
-        if (k < g.K && live) {
-          const _Float16* p = g.H + (size_t)kc * g.ld + m;
-          if (whole) h = *(const half8*)p;
-          else
+      for (int i = 0; i < NL; ++i) h[i] = s_h[i][tid];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (m + e < g.M) h[e] = p[e];
-        }
-      } else {
-        h = load_h(i);
-      }
-      finish(i, h, gamma_of(i));
+      for (int i = NL; i < NCH; ++i) h[i] = half8{0, 0, 0, 0, 0, 0, 0, 0};      // (rows behind K)
+      second_pass(NCH);
     }
-  }
+  } else
+    for (int i0 = 0; i0 < n_ch; i0 += NG) {
+      load_gamma(i0, gam);
+      if (NORM && g.H) {                 // this lane's own stores (X or R may be the same buffer, and are gone then)
+#pragma unroll
+        for (int i = 0; i < NG; ++i) h[i] = load_x(g.H, i0 + i);
+      } else {
+        load_h(i0, h);
+      }
+      second_pass(i0);
+    }
 }
 
+template <bool NORM, int TOK, int NT, int NCH, int NL = 0>
+hipError_t run_norm(const NormArgs& g, hipStream_t stream) {
+  const int per = (lines_of(g.M) + 7) / 8;
+  return launch_kernel(norm_kernel<NORM, TOK, NT, NCH, NL>, dim3(8 * per * (64 / TOK)), dim3(NT), stream, g);
+}
+
+#ifndef TUNE
+// Tokens per workgroup: 8 while that is at most one workgroup per CU (few rows of a token per lane and every CU at
+// work), 16 up to two, then 32, whose pieces of a row are half a line of memory; above 16384 whole lines.
+// Rows in registers as far as they fit, fewer lanes where they would have nothing to do.  us with 8 / 16 / 32 tokens (residual, int8
+// output, same buffers): 768 rows, 2048 tokens 6.5 / 7.0 / 8.1, 4096 tokens 8.8 / 8.1 / 9.3; 4096 rows, 16 tokens 6.4 / 9.5 / 13,
+// 1024 tokens 19 / 22 / 29, 4096 tokens 57 / 48 / 59, 8192 tokens 106 / 99 / 77; 1024 rows, 8192 tokens - / 24 / 20;
+// 4096 rows, 16384 tokens, 32 / 64 160 / 143, 8192 tokens 77 / 93.
 template <bool NORM>
 static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
-  const dim3 grid((unsigned)(((int64_t)g.M + TOK - 1) / TOK));
-  if (g.K <= 512) return launch_kernel(norm_kernel<NORM, 512, 4>, grid, dim3(512), stream, g);
-  if (g.K <= 1024) return launch_kernel(norm_kernel<NORM, 512, 8>, grid, dim3(512), stream, g);
-  if (g.K <= 2048) return launch_kernel(norm_kernel<NORM, 512, 16>, grid, dim3(512), stream, g);
-  return launch_kernel(norm_kernel<NORM, 512, 0>, grid, dim3(512), stream, g);
+  const int K = g.K;
+  if (g.M <= 2048 && K <= 8192) {
+    if (K <= 1024) return run_norm<NORM, 8, 512, 2>(g, stream);
+    if (K <= 2048) return run_norm<NORM, 8, 512, 4>(g, stream);
+    if (K <= 4096) return run_norm<NORM, 8, 1024, 4>(g, stream);
+    return run_norm<NORM, 8, 1024, 8>(g, stream);
+  }
+  if (g.M <= 4096 && K <= 4096) {
+    if (K <= 1024) return run_norm<NORM, 16, 1024, 2>(g, stream);
+    if (K <= 2048) return run_norm<NORM, 16, 1024, 4>(g, stream);
+    return run_norm<NORM, 16, 1024, 8>(g, stream);
+  }
+  if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
+  if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
+  // half of them in LDS; with a residual the registers do not suffice (8192 x 4096: 77 us read again, 82 kept)
+  if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);
+  if (g.M <= 16384 - 64) return run_norm<NORM, 32, 1024, 0>(g, stream);
+  return run_norm<NORM, 64, 1024, 0>(g, stream);
 }
 
 hipError_t launch_norm(bool norm, const NormArgs& g, hipStream_t stream) {
   return norm ? dispatch_norm<true>(g, stream) : dispatch_norm<false>(g, stream);
 }
+#endif
 
 }  // namespace twg

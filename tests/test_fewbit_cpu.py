@@ -248,6 +248,46 @@ def test_scaled_int8_product_refuses():
     assert _status(tw.tw_gemm_i8_scaled, P, 9, 16, w, P, P, P, 16) == 6
 
 
+def test_launch_calls_through_the_module_end_as_with_ctypes():
+    """Each argument in turn as an odd object: the same refusal or conversion on both routes (nothing is launched: the
+    weights are not uploaded and the calls without one get an invalid size)."""
+    from paper_2402_10876_amd import binding
+    tw.lib()
+    assert binding._call is not binding._Unbound
+    one = np.ones((40, 70), np.uint8)
+    w4 = tw.tw_pack_mx4_host(np.ones((40, 70), np.float16), one, 64)
+    w8 = tw.tw_pack_i8_host(np.ones((40, 70), np.int8), one, 64)
+    calls = [(tw.tw_rmsnorm, [P, P, P, 1e-6, 0, 5, 16, P, P, P, 16, P, 0]), (tw.tw_quant_i8, [P, 0, 5, 16, P, 16, P, 0]),
+             (tw.tw_quant_mx4, [P, 0, 5, 16, 0, P, P, 16, 0]), (tw.tw_gemm_i8_scaled, [P, 9, 16, w8, P, P, P, 16, 0]),
+             (tw.tw_gemm_mx4, [P, P, 9, 16, w4, P, 16, 0]), (tw.tw_gemm_mx4_grouped, [P, P, 9, 16, P, w4, P, 16, 0])]
+
+    def outcome(f, a):
+        try:
+            return f(*a)
+        except Exception as e:
+            return type(e), getattr(e, "status", None)
+    for f, good in calls:
+        for i, v in enumerate(good):
+            if v is w4 or v is w8:
+                continue
+            if i == {tw.tw_rmsnorm: 4, tw.tw_quant_i8: 1, tw.tw_quant_mx4: 1}.get(f):
+                odds = [v, None, True and 0, 0.0, "8", -1, 1 << 40]        # stays a size that is refused
+            else:
+                odds = [v, None, True, 8.0, "8", np.int64(8), -1, 1 << 31, 1 << 64]
+            for o in odds:
+                a = list(good)
+                a[i] = o
+                got = outcome(f, a)
+                call, binding._call = binding._call, binding._Unbound
+                try:
+                    want = outcome(f, a)
+                finally:
+                    binding._call = call
+                assert got == want, (f.__name__, i, o)
+    m = binding._call
+    assert m.rmsnorm(1) is None and m.quant_mx4(0, 1) is None and m.gemm_mx4(0, 0, 1, 16, None, 0, 8, 0) is None
+
+
 def test_row_count_check_of_the_masked_definition():
     """acts() holds what its users rely on."""
     x = acts(1, 9, 50)

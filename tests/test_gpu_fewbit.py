@@ -72,6 +72,24 @@ def test_norm(M, K):
     _check_norm(X, R, None, 1e-6, i8=False, f16=True, H=False)
 
 
+@pytest.mark.parametrize("M,K", [(2049, 64), (2500, 1100), (2200, 2100), (4097, 40), (4100, 1030), (4098, 2050), (8200, 300),
+                                 (16321, 2049), (16500, 2049), (16450, 96)])
+def test_norm_and_quantiser_of_many_tokens(M, K):
+    """Every number of tokens per workgroup, with a ragged last one."""
+    import torch
+    print(f"many tokens M={M} K={K}", flush=True)
+    X, R = acts(M + K, M, K), acts(M + K + 1, M, K, 3.0)
+    X[M - 2, K // 2] = np.inf
+    _check_norm(X, R, None, 1e-5, i8=True, f16=True)
+    q, scale = ofb.quant_i8(X)
+    Xd, ldq = dev_km(X, up(M, 8)), up(M, 16)
+    Q, s = torch.full((K, ldq), 99, dtype=torch.int8, device="cuda"), torch.zeros((M,), device="cuda")
+    tw.tw_quant_i8(Xd.data_ptr(), M, K, up(M, 8), Q.data_ptr(), ldq, s.data_ptr(), _stream())
+    assert np.array_equal(Q.cpu().numpy()[:, :M].T, q) and (Q[:, M:] == 99).all()
+    s = s.cpu().numpy()
+    assert np.array_equal(np.isnan(s), np.isnan(scale)) and (np.abs(np.nan_to_num(s - scale)) <= 2.0 ** -23 * np.nan_to_num(scale)).all()
+
+
 @pytest.mark.parametrize("alias", ["X", "R"])
 @pytest.mark.parametrize("K", [300, 5000])
 def test_norm_in_place_and_wider_strides(alias, K):
