@@ -259,22 +259,18 @@ tw_status tw_pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* ti
 // The parts of a microscaled 4-bit image in one allocation, 256-byte aligned each.
 static tw_status upload_mx4(tw_handle_t h, int dev) {
   twg::Mx4Image& d = h->mx4;
-  const void* src[7] = {d.tiles.data(), d.member_tile.data(), d.member_col.data(), d.blocks.data(), d.col_idx.data(),
-                        d.zero_cols.data(), d.vals.data()};
-  const size_t bytes[7] = {d.tiles.size() * sizeof(twg::Mx4Tile), d.member_tile.size() * 4, d.member_col.size() * 4,
-                           d.blocks.size() * 2, d.col_idx.size() * 4, d.zero_cols.size() * 4, d.vals.size()};
+  const void* src[6] = {d.tiles.data(), d.blocks.data(), d.col_idx.data(), d.zero_cols.data(), d.vals.data(), d.scales.data()};
+  const size_t bytes[6] = {d.tiles.size() * sizeof(twg::Mx4Tile), d.blocks.size() * 2, d.col_idx.size() * 4,
+                           d.zero_cols.size() * 4, d.vals.size(), d.scales.size()};
   size_t total = 0;
-  for (int i = 0; i < 7; ++i) {
+  for (int i = 0; i < 6; ++i) {
     d.off[i] = total;
     total += (bytes[i] + 255) / 256 * 256;
   }
-  d.off_scales = total;
-  total += (d.scales.size() + 255) / 256 * 256;
   void* blob = nullptr;
   if (hipMalloc(&blob, total) != hipSuccess) { (void)hipGetLastError(); return TW_ERR_ALLOC; }
-  bool ok = d.scales.empty() ||
-            hipMemcpy((char*)blob + d.off_scales, d.scales.data(), d.scales.size(), hipMemcpyHostToDevice) == hipSuccess;
-  for (int i = 0; ok && i < 7; ++i)
+  bool ok = true;
+  for (int i = 0; ok && i < 6; ++i)
     ok = !bytes[i] || hipMemcpy((char*)blob + d.off[i], src[i], bytes[i], hipMemcpyHostToDevice) == hipSuccess;
   if (!ok) {
     (void)hipGetLastError();
@@ -876,13 +872,14 @@ static tw_status gemm_mx4_launch(const void* Q, const void* S, int M, int ldq, c
   twg::GemmMx4Args g{};
   g.Q = (const uint8_t*)Q; g.S = (const uint8_t*)S; g.C = (_Float16*)C; g.M = M; g.ldq = ldq; g.ldc = ldc;
   g.tiles = (const twg::Mx4Tile*)(p + d.off[0]);
-  g.member_tile = (const int32_t*)(p + d.off[1]); g.member_col = (const int32_t*)(p + d.off[2]);
-  g.blocks = (const uint16_t*)(p + d.off[3]);
-  g.col_idx = (const int32_t*)(p + d.off[4]); g.zero_cols = (const int32_t*)(p + d.off[5]);
-  g.vals = (const uint8_t*)(p + d.off[6]); g.wscale = (const uint8_t*)(p + d.off_scales);
+  g.blocks = (const uint16_t*)(p + d.off[1]);
+  g.col_idx = (const int32_t*)(p + d.off[2]); g.zero_cols = (const int32_t*)(p + d.off[3]);
+  g.vals = (const uint8_t*)(p + d.off[4]); g.wscale = (const uint8_t*)(p + d.off[5]);
+  g.list_len = d.list_len;
   g.offsets = offsets;
-  g.n_members = offsets ? (int)d.member_tile.size() - 1 : 1;
-  g.n_tiles = offsets ? d.max_member_tiles : (int)d.tiles.size();
+  g.n_members = offsets ? d.n_members : 1;
+  g.member_n = h->N / g.n_members;
+  g.n_tiles = offsets ? d.n_tiles : d.n_members * d.n_tiles;
   const hipError_t e = twg::launch_gemm_mx4(h->G, g, (hipStream_t)stream);
   if (e == hipErrorInvalidValue) return TW_ERR_UNSUPPORTED;
   return e == hipSuccess ? TW_OK : TW_ERR_HIP;

@@ -34,14 +34,14 @@ struct GemmMx4Args {
   _Float16* C;                   // N x M, element (m, n) at C[n*ldc + m]
   int M, ldq, ldc;
   const Mx4Tile* tiles;
-  const int32_t *member_tile, *member_col;
   const uint16_t* blocks;
   const int32_t *col_idx, *zero_cols;
   const uint8_t *vals, *wscale;
-  int n_tiles;                   // grouped: most tiles of a member
+  int list_len;                  // entries of `blocks` per tile
+  int n_tiles;                   // grouped: of a member
   int n_mtiles;
   const int32_t* offsets;        // grouped: n_members + 1 first tokens, else null
-  int n_members;
+  int n_members, member_n;       // grouped: columns of a member
 };
 hipError_t launch_gemm_mx4(int G, GemmMx4Args g, hipStream_t stream);
 

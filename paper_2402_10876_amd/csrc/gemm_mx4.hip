@@ -32,10 +32,26 @@ __device__ __forceinline__ floatx16 mfma4(int4v a, int4v b, floatx16 c, int sa, 
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(a), widen(b), c, 4, 4, 0, sa, J, sb);
 }
 
+// Sum over the lanes up to the own one: inside rows of 16 lanes, then the rows' totals handed on (no LDS).
+__device__ __forceinline__ int prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);        // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // lane 15 of a row to the next row (rows 1 and 3)
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // lane 31 to rows 2 and 3
+  return x;
+}
+
 // The tokens of M-tile mt when they are shared out by expert: expert e owns [offsets[e], offsets[e+1]) (cut to [0, M); an
-// end in front of its start: none) in tiles of TM that start on a multiple of 8.  Every wave finds it by itself.
+// end in front of its start: none) in tiles of TM that start on a multiple of align_of(TM).  Every wave finds it by itself.
+// Tiles of 64 tokens and more start on lines of C (8 experts, 8192 tokens x 1024 columns: 1.25 times the time of one range with starts on 16 bytes,
+// 1.03 with lines), smaller ones on 16 bytes, so that an expert of few tokens has one tile.
 struct Range { int e, m0, lo, hi; };
-__device__ __forceinline__ bool find_range(const GemmMx4Args& g, int mt, int TM, int lane, Range& r) {
+constexpr int align_of(int TM) { return TM >= 64 ? 64 : 8; }
+template <int TM>
+__device__ __forceinline__ bool find_range(const GemmMx4Args& g, int mt, int lane, Range& r) {
+  constexpr int MASK = ~(align_of(TM) - 1);
   int before = 0;
   for (int c = 0; c < g.n_members; c += 64) {
     const int e = c + lane;
@@ -44,20 +60,15 @@ __device__ __forceinline__ bool find_range(const GemmMx4Args& g, int mt, int TM,
       a = min(max(g.offsets[e], 0), g.M);
       b = min(max(g.offsets[e + 1], 0), g.M);
     }
-    const int tiles = b > a ? (b - (a & ~7) + TM - 1) / TM : 0;
-    int incl = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int x = __shfl_up(incl, d);
-      if (lane >= d) incl += x;
-    }
+    const int tiles = b > a ? (b - (a & MASK) + TM - 1) / TM : 0;
+    const int incl = prefix_sum(tiles);
     const unsigned long long hit = __ballot(before + incl > mt);
     if (hit) {
       const int f = __ffsll((long long)hit) - 1;
       const int start = before + __builtin_amdgcn_readlane(incl - tiles, f);
       const int af = __builtin_amdgcn_readlane(a, f);
       r.e = c + f;
-      r.m0 = (af & ~7) + (mt - start) * TM;
+      r.m0 = (af & MASK) + (mt - start) * TM;
       r.lo = max(af, r.m0);
       r.hi = __builtin_amdgcn_readlane(b, f);
       return true;
@@ -70,7 +81,7 @@ __device__ __forceinline__ bool find_range(const GemmMx4Args& g, int mt, int TM,
 }  // namespace
 
 template <int GB, int MB, int NB, int WM, int WN, int WK, int D>
-__global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gemm_mx4_kernel(GemmMx4Args g) {
+__global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB == 8 ? 2 : 1)) void gemm_mx4_kernel(GemmMx4Args g) {
   constexpr int NT = 64 * WM * WN * WK;
   constexpr int TM = 32 * MB * WM, CB = NB * WN;            // tokens, column blocks of the workgroup
   constexpr int SUB = GB / CB;                              // workgroups per tile of columns
@@ -78,8 +89,13 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
   // staged output: WK = 1 a wave's halves [n][m], else the waves' fp32 partial sums [wave][n][m]
   constexpr int PITCH = WK == 1 ? 32 * MB * 2 + 16 : 36 * 4;
   constexpr int AREA = 32 * NB * PITCH;
-  __shared__ __attribute__((aligned(16))) char stage[WM * WN * WK * AREA];
-  __shared__ uint16_t list[MAX_BLOCKS];
+  // (the list of blocks lies in front of it: 256 x 128 tiles of four waves come twice into a CU's LDS without the 8 KiB
+  // beside them, 12.9 against 15.8 us for 1024 x 4096, half, at M = 4096)
+  constexpr int STAGE = WM * WN * WK * AREA;
+  __shared__ __attribute__((aligned(16))) char stage[STAGE > MAX_BLOCKS * 2 ? STAGE : MAX_BLOCKS * 2];
+  uint16_t* list = (uint16_t*)stage;
+  constexpr int ZL = 64;                                    // pruned columns whose numbers are fetched with the list
+  __shared__ int cols[CB * 32], zeros[ZL];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -91,33 +107,30 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
   const int sub = (lid - mt * nt) % SUB;
 
   Range r{0, mt * TM, mt * TM, g.M};
-  int col_base = 0;
   if (g.offsets) {
-    if (!find_range(g, mt, TM, lane, r)) return;
-    col_base = g.member_col[r.e];
-    t += g.member_tile[r.e];
-    if (t >= g.member_tile[r.e + 1]) return;
+    if (!find_range<TM>(g, mt, lane, r)) return;
+    t += r.e * g.n_tiles;
   }
+  const int col_base = r.e * g.member_n;
   const int m0 = r.m0, m_end = min(r.hi, m0 + TM);
+  // the tile's record, its list of blocks (whatever is in use of it) and its columns in one round trip
   const Mx4Tile tile = g.tiles[t];
+  const uint16_t* blocks = g.blocks + (size_t)t * g.list_len;
+  const int32_t* col_idx = g.col_idx + (size_t)t * (GB * 32) + sub * CB * 32;
+  constexpr int CPT = (CB * 32 + NT - 1) / NT;
+  const u32x4 l0 = tid * 8 < g.list_len ? *(const u32x4*)(blocks + tid * 8) : u32x4{0u, 0u, 0u, 0u};
+  int c0[CPT];
+#pragma unroll
+  for (int i = 0; i < CPT; ++i) c0[i] = col_idx[min(tid + i * NT, CB * 32 - 1)];
+  if (tid * 8 < g.list_len) *(u32x4*)(list + tid * 8) = l0;
+#pragma unroll
+  for (int i = 0; i < CPT; ++i)
+    if (tid + i * NT < CB * 32) cols[tid + i * NT] = c0[i];
+  const int z0 = tile.zero_beg + (int)((int64_t)(tile.zero_end - tile.zero_beg) * sub / SUB);
+  const int nz = tile.zero_beg + (int)((int64_t)(tile.zero_end - tile.zero_beg) * (sub + 1) / SUB) - z0;
+  if (tid < min(nz, ZL)) zeros[tid] = g.zero_cols[z0 + tid];
+  for (int i = (NT + tid) * 8; i < g.list_len; i += NT * 8) *(u32x4*)(list + i) = *(const u32x4*)(blocks + i);
   const int ns = tile.steps;
-  for (int i = tid; i < 2 * ns; i += NT) list[i] = g.blocks[2 * tile.step0 + i];
-
-  // pruned columns: 0
-  {
-    const int p0 = (r.lo - m0) >> 3, np = ((m_end - m0 + 7) >> 3) - p0;
-    const int nz = tile.zero_end - tile.zero_beg;
-    const int z0 = tile.zero_beg + (int)((int64_t)nz * sub / SUB), z1 = tile.zero_beg + (int)((int64_t)nz * (sub + 1) / SUB);
-    for (int i = tid; i < (z1 - z0) * np; i += NT) {
-      const int z = i / np, m = m0 + (p0 + i - z * np) * 8;
-      _Float16* to = g.C + (size_t)(g.zero_cols[z0 + z] - col_base) * g.ldc + m;
-      if (m >= r.lo && m + 8 <= m_end) *(u32x4*)to = u32x4{0u, 0u, 0u, 0u};
-      else
-        for (int e = 0; e < 8; ++e)
-          if (m + e >= r.lo && m + e < m_end) to[e] = (_Float16)0.f;
-    }
-  }
-  __syncthreads();
 
   floatx16 acc[MB][NB];
 #pragma unroll
@@ -137,7 +150,13 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
   const uint8_t* ws = g.wscale + ((size_t)tile.step0 * 64 + lane) * GB;
   const uint32_t ldq = (uint32_t)g.ldq;
   const int half = lane >> 5;
-  auto load = [&](int s, Step& x) {
+  auto load_w = [&](int s, Step& x) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) x.b[j] = *(const int4v*)(wv + (size_t)s * (GB * 1024) + j * 1024);
+    if constexpr (GB == 4) x.sb = *(const int*)(ws + (size_t)s * 256);
+    else x.sb = *(const uint16_t*)(ws + (size_t)s * 128);
+  };
+  auto load_a = [&](int s, Step& x) {
     const uint32_t b = list[2 * s + half];
     const uint8_t* q = g.Q + (uint64_t)b * ldq * 16u;
     const uint8_t* sc = g.S + (uint64_t)b * ldq;
@@ -146,11 +165,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
       x.a[i] = *(const int4v*)(q + tok[i] * 16u);
       x.sa[i] = sc[tok[i]];
     }
-#pragma unroll
-    for (int j = 0; j < NB; ++j) x.b[j] = *(const int4v*)(wv + (size_t)s * (GB * 1024) + j * 1024);
-    if constexpr (GB == 4) x.sb = *(const int*)(ws + (size_t)s * 256);
-    else x.sb = *(const uint16_t*)(ws + (size_t)s * 128);
   };
+  auto load = [&](int s, Step& x) { load_a(s, x); load_w(s, x); };
   auto multiply = [&](const Step& x) {
     const int sb = (int)((uint32_t)x.sb >> (8 * nb0));
 #pragma unroll
@@ -164,10 +180,15 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
 
   // D steps under way: the wave's steps are wk, wk + WK, .. (n of them)
   const int n = (ns - wk + WK - 1) / WK;
+  Step st[D];
   if (n > 0) {
-    Step st[D];
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(wk + min(d, n - 1) * WK, st[d]);
+    for (int d = 0; d < D; ++d) load_w(wk + min(d, n - 1) * WK, st[d]);
+  }
+  __syncthreads();
+  if (n > 0) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) load_a(wk + min(d, n - 1) * WK, st[d]);
     int i = 0;
     for (; i + 2 * D <= n; i += D)
 #pragma unroll
@@ -187,6 +208,26 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
       if (i + d < n) multiply(st[d]);
   }
 
+  const bool lines = TM >= 64 && r.lo == m0 && m_end == m0 + TM;        // whole lines of C
+  auto store = [&](int col, int m, half8 v) {
+    if (col < 0) return;
+    _Float16* to = g.C + (size_t)(col - col_base) * g.ldc + m;
+    if (m >= r.lo && m + 8 <= m_end) {
+      if (lines) __builtin_nontemporal_store(v, (half8*)to);
+      else *(half8*)to = v;
+    } else
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (m + e >= r.lo && m + e < m_end) to[e] = v[e];
+  };
+  // the workgroup's share of the pruned columns: 0 (here, where no load waits behind these stores)
+  const int p0 = (r.lo - m0) >> 3, np = ((m_end - m0 + 7) >> 3) - p0;
+  for (int i = tid; i < nz * np; i += NT) {
+    const int z = i / np;
+    store(z < ZL ? zeros[z] : g.zero_cols[z0 + z], m0 + (p0 + i - z * np) * 8, half8{0, 0, 0, 0, 0, 0, 0, 0});
+  }
+
+  __syncthreads();                          // everybody is done with the list
   // acc[i][j][x] is token 8 (x / 4) + 4 (lane / 32) + x % 4, column lane % 32 of block (i, j)
   char* mine = stage + wave * AREA;
 #pragma unroll
@@ -209,16 +250,6 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB >= 8 ? 2 : 1)) void gem
         }
       }
   __syncthreads();
-  auto store = [&](int col, int m, half8 v) {
-    if (col < 0) return;
-    _Float16* to = g.C + (size_t)(col - col_base) * g.ldc + m;
-    if (m >= r.lo && m + 8 <= m_end) __builtin_nontemporal_store(v, (half8*)to);
-    else
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (m + e >= r.lo && m + e < m_end) to[e] = v[e];
-  };
-  const int32_t* cols = g.col_idx + (size_t)t * (GB * 32) + sub * CB * 32;
   if constexpr (WK == 1) {
     constexpr int PPR = 4 * MB;           // pieces of 8 tokens per row of the wave's tile
 #pragma unroll
@@ -252,7 +283,7 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
   int64_t mtiles = ((int64_t)g.M + TM - 1) / TM;
   if (g.offsets) {                        // most tiles that ranges of M tokens together can be cut into
     const int64_t met = g.n_members < g.M ? g.n_members : g.M;
-    mtiles = ((int64_t)g.M + met * (TM + 6)) / TM;
+    mtiles = ((int64_t)g.M + met * (TM - 1 + align_of(TM) - 1)) / TM;
   }
   const int64_t grid = mtiles * g.n_tiles * SUB;
   if (grid * (64 * WM * WN * WK) > 0xffffffffll) return hipErrorInvalidValue;
@@ -260,17 +291,57 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
   return launch_kernel(gemm_mx4_kernel<GB, MB, NB, WM, WN, WK, D>, dim3((unsigned)grid), dim3(64 * WM * WN * WK), stream, g);
 }
 
+#ifndef TUNE
+// Tile shapes, tokens x columns (waves, how the work is shared), us per launch in a captured stream of launches, operands from
+// HBM, K x N and the share of the blocks kept:
+//   R 256 x 128 (2)       wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
+//   Q 256 x 128 (4)       wave tiles of 64 x 128: more waves to hide the ends of short lists
+//   P 128 x 128 (4)
+//   W  64 x 128 (2)
+//   U  32 x 128 (2)
+//   S  32 x 32 (4 on shares of the list), S2 64 x 32 (2 x 4)
+// Large: 4096 x 4096, all, M = 8192 R 78.6, Q 84.4, P 110; half, R 50.4, Q 48.3; 1024 x 4096, half, M = 4096 Q 12.9, P 13.5, R 15+.
+// From 384 tiles of 256 rows on: fewer leave CUs idle (2048 x 1024, half, M = 8192, 256 tiles: P 10.4, Q 10.8; 1024 x 1024
+// P 7.6, Q 8.9).  From 200 tiles of P on: 2048 x 2048, half, M = 2048 P 7.5, U 7.5; 4096 x 4096, half, M = 1024 P 10.7,
+// U 11.9; 1024 x 4096, half, M = 512 (128 tiles) P 5.6, U 5.4; 1024 x 1024, M = 1024 P 4.7, U 3.7.
+// Lists shared among waves where tiles of 64 rows would be fewer than 160 and a list is long: 4096 x 4096, half, M = 128
+// S2 5.2, S 6.0, U 7.6; all, M = 256 S2 10.5, U 12.0; 4096 x 1024, all, M = 512 S2 6.9, U 10; up to 256 tiles of S it has
+// the shortest way: 1024 x 1024, half, M = 256 S 3.0, S2 3.1, U 3.4; 4096 x 4096, M = 1 S 3.7, S2 4.3.
+// By expert, where ranges end inside tiles: 2048 x 1024, half, 8 experts, M = 8192 W 13.7, U 15.4, P 16.1; M = 2048 U 8.0,
+// W 9.0; M = 512 S 6.2, U 7+; 1024 x 1024, 32 experts, M = 4000 W 10.0, U 10.6; M = 1000 U 7.8, S 9.7.
 template <int GB>
 static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
-  // few tokens (per expert): 32 x 32 tiles whose eight waves share out the steps
-  const int64_t tokens = g.offsets ? (int64_t)g.M / g.n_members : g.M;
-  if (tokens <= 64) return launch_mx4<GB, 1, 1, 1, 1, 8, 2>(g, stream);
-  if constexpr (GB == 4) return launch_mx4<4, 2, 2, 2, 2, 1, 3>(g, stream);
-  else return launch_mx4<2, 2, 1, 2, 2, 1, 3>(g, stream);
+  const int64_t M = g.M, n = ((int64_t)g.n_tiles * GB + 3) / 4;        // column tiles of 128
+  const int steps = g.list_len / 2;
+  enum { R, Q, P, W, U, S, S2 } shape;
+  if (g.offsets && M / g.n_members < 2048) {
+    const int64_t met = g.n_members < M ? g.n_members : M;
+    shape = (M / 32 + met) * n * 4 <= 1024 ? S : (M / 64 + met) * n < 512 ? U : W;
+  } else {
+    auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
+    if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles(32) * 4 <= 256 ? S : S2;
+    else if (tiles(256) >= 384) shape = steps >= 32 ? R : Q;
+    else shape = tiles(128) >= 200 ? P : U;
+  }
+  if (shape == S) return launch_mx4<GB, 1, 1, 1, 1, 4, 4>(g, stream);
+  if (shape == S2) return launch_mx4<GB, 1, 1, 2, 1, 4, 4>(g, stream);
+  if constexpr (GB == 4) {
+    if (shape == R) return launch_mx4<4, 4, 4, 2, 1, 1, 3>(g, stream);
+    if (shape == Q) return launch_mx4<4, 2, 4, 4, 1, 1, 2>(g, stream);
+    if (shape == P) return launch_mx4<4, 2, 2, 2, 2, 1, 4>(g, stream);
+    if (shape == W) return launch_mx4<4, 2, 2, 1, 2, 1, 3>(g, stream);
+    return launch_mx4<4, 1, 2, 1, 2, 1, 4>(g, stream);
+  } else {      // tiles of 64 columns: R and Q 512 x 64 (4 waves), P 256 x 64 (4), W 64 x 64 (1), U 32 x 64 (2)
+    if (shape == R || shape == Q) return launch_mx4<2, 4, 2, 4, 1, 1, 2>(g, stream);
+    if (shape == P) return launch_mx4<2, 2, 2, 4, 1, 1, 4>(g, stream);
+    if (shape == W) return launch_mx4<2, 2, 2, 1, 1, 1, 4>(g, stream);
+    return launch_mx4<2, 1, 1, 1, 2, 1, 4>(g, stream);
+  }
 }
 
 hipError_t launch_gemm_mx4(int G, GemmMx4Args g, hipStream_t stream) {
   return G == 128 ? dispatch_mx4<4>(g, stream) : dispatch_mx4<2>(g, stream);
 }
+#endif
 
 }  // namespace twg

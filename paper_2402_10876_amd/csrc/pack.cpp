@@ -285,51 +285,60 @@ static void build_mx4_image(tw_handle_s* h) {
   const int G = h->G, GB = G / 32;
   std::vector<int32_t> members = h->member_n;
   if (members.empty()) members.assign(1, h->N);
-  d.member_tile.assign(1, 0); d.member_col.assign(1, 0);
   std::vector<uint8_t> is_kept(h->N, 0);
   for (int32_t c : h->col_idx) is_kept[c] = 1;
-  int64_t step = 0;
-  int t = 0;
-  for (int32_t n : members) {                  // tiles
-    const int first = (int)d.tiles.size(), col1 = d.member_col.back() + n;
-    const int z0 = (int)d.zero_cols.size();
-    for (int c = d.member_col.back(); c < col1; ++c)
-      if (!is_kept[c]) d.zero_cols.push_back(c);
-    const int zeros = (int)d.zero_cols.size() - z0;
+  // tiles of the members in the logical form, and the longest list
+  std::vector<int> first(1, 0);
+  int col1 = 0, most = 0;
+  for (int32_t n : members) {
+    col1 += n;
+    int t = first.back();
     for (; t < h->n_tiles && h->col_idx[h->tile_col_off[t]] < col1; ++t) {
-      Mx4Tile r{};
+      int blocks = 0;
+      for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1]; ++i) blocks += h->row_idx[i] % MX4_BLOCK == 0;
+      most = std::max(most, blocks);
+    }
+    first.push_back(t);
+  }
+  d.n_members = (int)members.size();
+  d.n_tiles = 1;
+  for (int e = 0; e < d.n_members; ++e) d.n_tiles = std::max(d.n_tiles, first[e + 1] - first[e]);
+  d.list_len = (most + 7) / 8 * 8;
+  const size_t total = (size_t)d.n_members * d.n_tiles;
+  d.tiles.assign(total, Mx4Tile{});
+  d.blocks.assign(total * d.list_len, 0);
+  d.col_idx.assign(total * G, -1);
+  int64_t step = 0;
+  int col0 = 0;
+  for (int e = 0; e < d.n_members; ++e) {
+    const int z0 = (int)d.zero_cols.size();
+    for (int c = col0; c < col0 + members[e]; ++c)
+      if (!is_kept[c]) d.zero_cols.push_back(c);
+    col0 += members[e];
+    const int zeros = (int)d.zero_cols.size() - z0;
+    for (int i = 0; i < d.n_tiles; ++i) {
+      const size_t at = (size_t)e * d.n_tiles + i;
+      Mx4Tile& r = d.tiles[at];
+      r.zero_beg = z0 + (int)((int64_t)zeros * i / d.n_tiles);
+      r.zero_end = z0 + (int)((int64_t)zeros * (i + 1) / d.n_tiles);
       r.step0 = step;
-      for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1]; ++i)
-        if (h->row_idx[i] % MX4_BLOCK == 0) d.blocks.push_back((uint16_t)(h->row_idx[i] / MX4_BLOCK));
-      if (d.blocks.size() % 2) d.blocks.push_back(d.blocks.back());
-      step = (int64_t)d.blocks.size() / 2;
-      r.steps = (int32_t)(step - r.step0);
-      d.tiles.push_back(r);
-      for (int j = 0; j < G; ++j) {
-        const int c = h->tile_col_off[t] + j;
-        d.col_idx.push_back(c < h->tile_col_off[t + 1] ? h->col_idx[c] : -1);
-      }
+      const int t = first[e] + i;
+      if (t >= first[e + 1]) continue;
+      uint16_t* list = d.blocks.data() + at * d.list_len;
+      int n = 0;
+      for (int k = h->tile_k_off[t]; k < h->tile_k_off[t + 1]; ++k)
+        if (h->row_idx[k] % MX4_BLOCK == 0) list[n++] = (uint16_t)(h->row_idx[k] / MX4_BLOCK);
+      if (n % 2) { list[n] = list[n - 1]; ++n; }
+      r.steps = n / 2;
+      step += r.steps;
+      for (int c = h->tile_col_off[t]; c < h->tile_col_off[t + 1]; ++c) d.col_idx[at * G + c - h->tile_col_off[t]] = h->col_idx[c];
     }
-    if ((int)d.tiles.size() == first) {
-      Mx4Tile r{};
-      r.step0 = step;
-      d.tiles.push_back(r);
-      d.col_idx.insert(d.col_idx.end(), G, -1);
-    }
-    const int tiles = (int)d.tiles.size() - first;
-    for (int i = 0; i < tiles; ++i) {
-      d.tiles[first + i].zero_beg = z0 + (int)((int64_t)zeros * i / tiles);
-      d.tiles[first + i].zero_end = z0 + (int)((int64_t)zeros * (i + 1) / tiles);
-    }
-    d.max_member_tiles = std::max(d.max_member_tiles, tiles);
-    d.member_tile.push_back((int32_t)d.tiles.size());
-    d.member_col.push_back(col1);
   }
   d.vals.assign((size_t)step * GB * 1024, 0);
   d.scales.assign((size_t)step * GB * 64, (uint8_t)MX4_ONE);
   int64_t s0 = 0;
   uint16_t top[128];
-  for (int tl = 0; tl < h->n_tiles; ++tl) {    // values (the tiles that keep nothing have no steps)
+  for (int tl = 0; tl < h->n_tiles; ++tl) {    // values (the tiles that fill up have no steps)
     const int w = h->tile_col_off[tl + 1] - h->tile_col_off[tl];
     const uint16_t* v = h->values.data() + h->val_off[tl];
     int b = 0;

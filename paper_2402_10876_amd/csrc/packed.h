@@ -70,22 +70,21 @@ struct ImageLayout { size_t bytes[IMG_PARTS], off[IMG_PARTS], total; };
 // Device image of a microscaled 4-bit weight (dtype TW_DTYPE_MX4).  A tile's kept blocks of 32 rows go two by two through
 // v_mfma_scale_f32_32x32x64_f8f6f4: a step is two blocks (the second one zeros where the number is odd).
 struct Mx4Tile {               // one record per tile, read by a workgroup as it starts
-  int64_t step0;               // first step: of `blocks` (two each), `vals` and `scales`
+  int64_t step0;               // first step: of `vals` and `scales`
   int32_t steps;
   int32_t zero_beg, zero_end;  // pruned columns that the tile's workgroups clear (zero_cols)
   int32_t pad[3];
 };
 struct Mx4Image {
-  std::vector<Mx4Tile> tiles;          // per member its tiles, at least one (a member that keeps nothing has a tile of no steps)
-  std::vector<int32_t> member_tile;    // n_members + 1: tiles of a member
-  std::vector<int32_t> member_col;     // n_members + 1: columns of a member
-  std::vector<uint16_t> blocks;        // 2 per step: number of the block (a repeated one where the number is odd)
+  int32_t n_members = 1, n_tiles = 1;  // tiles of a member, the same number for all (filled up with tiles of no steps)
+  int32_t list_len = 0;                // entries of a tile's list of blocks, a multiple of 8
+  std::vector<Mx4Tile> tiles;          // n_members * n_tiles
+  std::vector<uint16_t> blocks;        // list_len per tile, 2 per step: number of the block (a repeated one where the number is odd)
   std::vector<int32_t> col_idx;        // G per tile: original column, -1 = none
   std::vector<int32_t> zero_cols;
   std::vector<uint8_t> vals;           // per step and column block of 32: [lane][16 bytes], lane l = column l % 32, block l / 32
   std::vector<uint8_t> scales;         // per step: [lane][G / 32 bytes], byte j: column block j
-  int32_t max_member_tiles = 0;
-  size_t off[7] = {}, off_scales = 0;  // of the parts above in the device allocation, in this order; of `scales`
+  size_t off[6] = {};                  // of these six in the device allocation, in this order
 };
 
 }  // namespace twg

@@ -5,8 +5,8 @@
 // past 6 to 6; checked for every fp16 value against the definition).  Bound by memory: 2 bytes in and 17/32 out per value.
 //   K x M : a lane takes two neighbouring tokens, 32 loads of 4 bytes, all under way at once; a wave reads 256 bytes of
 //           each row and writes 2 KiB of codes in a run.
-//   M x K : a lane takes one block of a token, 64 bytes in a run; a wave is 8 tokens x 8 blocks, so that both
-//           the reads (512 bytes of a token) and the writes (128 bytes of a block row) are whole lines.
+//   M x K : a wave takes 16 blocks of 8 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
+//           collected in LDS so that the writes are whole lines (8 tokens of a block row) as well.
 #include <type_traits>
 
 #include "device_common.h"
@@ -28,18 +28,24 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   return (__float_as_uint(f) >> 23) - 2;
 }
 
+// 4 pairs of fp16 values (rows 2i, 2i+1) to 8 codes.
+__device__ __forceinline__ uint32_t encode8(const uint32_t (&x)[4], float scale) {
+  uint32_t o = 0;
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[0]), scale, 0);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[1]), scale, 1);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[2]), scale, 2);
+  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[3]), scale, 3);
+  return o;
+}
+
 // 16 pairs of fp16 values (rows 2i, 2i+1) to 32 codes; a block that is not finite gets zeros.
 __device__ __forceinline__ u32x4 encode(const uint32_t (&x)[16], uint32_t scale) {
   const float s = __uint_as_float((scale == MX4_NAN ? MX4_ONE : scale) << 23);
   u32x4 out;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t o = 0;
-    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[4 * i]), s, 0);
-    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[4 * i + 1]), s, 1);
-    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[4 * i + 2]), s, 2);
-    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, x[4 * i + 3]), s, 3);
-    out[i] = scale == MX4_NAN ? 0u : o;
+    const uint32_t w[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    out[i] = scale == MX4_NAN ? 0u : encode8(w, s);
   }
   return out;
 }
@@ -85,38 +91,68 @@ __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n
   }
 }
 
-// M x K.  One wave: 8 tokens x 8 blocks.
+// M x K.  One wave: TOK tokens x 16 blocks; four lanes hold a block of a token.
+template <int TOK>
 __global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks) {
+  __shared__ __attribute__((aligned(16))) uint32_t codes[4][16 * TOK * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = ((int)blockIdx.x * 4 + wave) * 8 + (lane & 7), b = (int)blockIdx.y * 8 + (lane >> 3);
-  if (m >= g.M || b >= n_blocks) return;
-  const int k0 = b * MX4_BLOCK, rows = g.K - k0;
-  const _Float16* x = g.X + (size_t)m * g.ldx + k0;
-  uint32_t v[16];
+  const int m0 = ((int)blockIdx.x * 4 + wave) * TOK, b0 = (int)blockIdx.y * 16;
+  if (m0 >= g.M) return;
+  const int k = b0 * MX4_BLOCK + lane * 8, left = g.K - k;         // values of the lane in front of K: left and more
+  const _Float16* x = g.X + (size_t)m0 * g.ldx + (left > 0 ? k : 0);
+  u32x4 v[TOK];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u32x4 w = {0u, 0u, 0u, 0u};
-    if (8 * i < rows) w = *(const u32x4*)(x + 8 * i);
+  for (int t = 0; t < TOK; ++t) v[t] = *(const u32x4*)(x + (size_t)min(t, g.M - 1 - m0) * g.ldx);
+  if (left < 8) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = 8 * i + 2 * j;
-      v[4 * i + j] = k + 1 < rows ? w[j] : k < rows ? w[j] & 0xffffu : 0u;
+    for (int t = 0; t < TOK; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[t][j] = 2 * j + 1 < left ? v[t][j] : 2 * j < left ? v[t][j] & 0xffffu : 0u;
+  }
+  uint32_t scales[TOK / 4] = {};
+#pragma unroll
+  for (int t = 0; t < TOK; ++t) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max_u16x2(top, v[t][j] & 0x7fff7fffu);
+    top = max(top & 0xffffu, top >> 16);
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, true));     // quad_perm [1,0,3,2]
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, true));     // quad_perm [2,3,0,1]
+    const uint32_t s = scale_byte(top);
+    scales[t / 4] |= s << (8 * (t % 4));
+    const float f = __uint_as_float((s == MX4_NAN ? MX4_ONE : s) << 23);
+    const uint32_t w[4] = {v[t][0], v[t][1], v[t][2], v[t][3]};      // (a bit cast of a vector's element takes the first one)
+    const uint32_t o = encode8(w, f);
+    codes[wave][((lane >> 2) * TOK + t) * 4 + (lane & 3)] = s == MX4_NAN ? 0u : o;
+  }
+  // (an area of the wave's own: LDS instructions of a wave are done in order)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < TOK / 4; ++i) {
+    const int p = i * 64 + lane, b = b0 + p / TOK, m = m0 + p % TOK;
+    const u32x4 c = *(const u32x4*)&codes[wave][p * 4];
+    if (b < n_blocks && m < g.M) *(u32x4*)(g.Q + ((size_t)b * g.ldq + m) * 16) = c;
+  }
+  const int b = b0 + (lane >> 2);
+  if ((lane & 3) == 0 && b < n_blocks) {
+    uint8_t* to = g.S + (size_t)b * g.ldq + m0;
+#pragma unroll
+    for (int i = 0; i < TOK / 4; ++i) {
+      if (m0 + 4 * i + 4 <= g.M) *(uint32_t*)(to + 4 * i) = scales[i];
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (m0 + 4 * i + e < g.M) to[4 * i + e] = (uint8_t)(scales[i] >> (8 * e));
     }
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = max_u16x2(top, v[i] & 0x7fff7fffu);
-  const uint32_t s = scale_byte(max(top & 0xffffu, top >> 16));
-  const size_t at = (size_t)b * g.ldq + m;
-  *(u32x4*)(g.Q + at * 16) = encode(v, s);
-  g.S[at] = (uint8_t)s;
 }
 
 hipError_t launch_quant_mx4(bool km, const QuantMx4Args& g, hipStream_t stream) {
   const int nb = (g.K + MX4_BLOCK - 1) / MX4_BLOCK;
   if (km)
     return launch_kernel(quant_mx4_km_kernel, dim3((unsigned)(((int64_t)g.M + 127) / 128), (nb + 3) / 4), dim3(256), stream, g, nb);
-  return launch_kernel(quant_mx4_mk_kernel, dim3((unsigned)(((int64_t)g.M + 31) / 32), (nb + 7) / 8), dim3(256), stream, g, nb);
+  return launch_kernel(quant_mx4_mk_kernel<8>, dim3((unsigned)(((int64_t)g.M + 31) / 32), (nb + 15) / 16), dim3(256), stream, g, nb);
 }
 
 }  // namespace twg

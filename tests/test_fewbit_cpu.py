@@ -144,7 +144,7 @@ int main() {
     if (twg::pack_mx4_host(B.data(), mask.data(), K, N, G, &b) != TW_OK) { ++fails; continue; }
     const tw_handle_s* parts[2] = {&a, &b};
     if (twg::concat_host(parts, 2, &c) != TW_OK) ++fails;
-    if (c.mx4.vals.size() != 2 * a.mx4.vals.size() || c.mx4.member_tile.size() != 3) ++fails;
+    if (c.mx4.vals.size() != 2 * a.mx4.vals.size() || c.mx4.n_members != 2) ++fails;
     std::vector<uint16_t> W((size_t)K * N);
     twg::unpack_host(&a, W.data(), nullptr);
     if (twg::pack_mx4_host(W.data(), mask.data(), K, N, G, &(b = tw_handle_s())) != TW_OK || b.mx4.vals != a.mx4.vals || b.mx4.scales != a.mx4.scales) ++fails;
