@@ -348,11 +348,13 @@ static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
     if (K <= 2048) return run_norm<NORM, 16, 1024, 4>(g, stream);
     return run_norm<NORM, 16, 1024, 8>(g, stream);
   }
-  if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
-  if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
-  // half of them in LDS; with a residual the registers do not suffice (8192 x 4096: 77 us read again, 82 kept)
-  if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);
-  if (g.M <= 16384 - 64) return run_norm<NORM, 32, 1024, 0>(g, stream);
+  if (g.M < 1 << 25) {                   // (2^32 threads in a grid: none of 32 tokens beyond 2^27 - 1)
+    if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
+    if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
+    // half of them in LDS; with a residual the registers do not suffice (8192 x 4096: 77 us read again, 82 kept)
+    if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);
+    if (g.M <= 16384 - 64) return run_norm<NORM, 32, 1024, 0>(g, stream);
+  }
   return run_norm<NORM, 64, 1024, 0>(g, stream);
 }
 

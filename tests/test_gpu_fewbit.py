@@ -141,6 +141,39 @@ def test_quant_i8(M, K):
     assert (np.abs(np.nan_to_num(s[:M] - scale)) <= 2.0 ** -23 * np.nan_to_num(scale)).all()
 
 
+def test_the_most_tokens():
+    """2^27 tokens of one or two values: the largest grids."""
+    import torch
+    M = 1 << 27
+    x = torch.randn((2, M), device="cuda", dtype=torch.float16)
+    Q = torch.zeros((2, M), dtype=torch.int8, device="cuda")
+    s = torch.zeros((M,), device="cuda")
+    print("most tokens: int8", flush=True)
+    tw.tw_quant_i8(x.data_ptr(), M, 2, M, Q.data_ptr(), M, s.data_ptr(), _stream())
+    top = x.float().abs().amax(0)
+    assert bool((Q.abs().amax(0) == 127 * (top > 0)).all()) and bool(((s * 127 - top).abs() <= 2.0 ** -22 * top).all())
+    assert bool((Q.float() * s - x.float()).abs().le(0.5001 * s).all())
+    del Q, top
+    print("most tokens: norm", flush=True)
+    Y = torch.zeros((2, M), dtype=torch.float16, device="cuda")
+    tw.tw_rmsnorm(x.data_ptr(), None, None, 1e-6, M, 2, M, None, Y.data_ptr(), None, 0, None, _stream())
+    want = x.float() / torch.sqrt((x.float() ** 2).mean(0) + 1e-6)
+    assert bool(((Y.float() - want).abs() <= (fu.STEP16 + 1e-5) * want.abs() + 2.0 ** -25).all())
+    del Y, want
+    print("most tokens: 4 bits", flush=True)
+    codes = torch.zeros((1, M, 16), dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((1, M), dtype=torch.uint8, device="cuda")
+    tw.tw_quant_mx4(x.data_ptr(), M, 2, M, tw.LAYOUT_KM, codes.data_ptr(), scale.data_ptr(), M, _stream())
+    at = torch.tensor([0, 1, M // 2 + 3, M - 2, M - 1], device="cuda")
+    c, e = ofb.mx4_quant(x[:, at].cpu().numpy())
+    assert np.array_equal(codes[0, at].cpu().numpy(), ofb.mx4_bytes(c)[0]) and np.array_equal(scale[0, at].cpu().numpy(), e[0])
+    p = tw.tw_pack_mx4(np.array([[1.0], [-2.0]], np.float16), np.ones((2, 1), np.uint8), 64)
+    C = torch.zeros((1, M), dtype=torch.float16, device="cuda")
+    tw.tw_gemm_mx4(codes.data_ptr(), scale.data_ptr(), M, M, p, C.data_ptr(), M, _stream())
+    v = ofb.mx4_values(c, e, 2)
+    assert np.array_equal(C[0, at].cpu().numpy(), (v[0] - 2 * v[1]).astype(np.float16))
+
+
 def test_quant_i8_every_ratio():
     """All pairs of small mantissas: quotients on and next to halves."""
     import torch
