@@ -31,6 +31,59 @@ __device__ __forceinline__ float settle(float g, float top, float n, float d) {
   return (x < edge || (x == edge && odd)) ? n - 1.f : n;
 }
 
+// What a token is finished with, from its sum of squares and its largest |g| (INF_BITS: not finite).
+struct Token { float inv, top, mul, scale; };
+template <bool NORM>
+__device__ __forceinline__ Token finish_token(float sum, uint32_t top, const NormArgs& g) {
+  Token t;
+  t.inv = 1.f;
+  if constexpr (NORM) t.inv = 1.f / sqrtf(sum / (float)g.K + g.eps);
+  const bool fine = top != 0 && top < INF_BITS;
+  t.top = __uint_as_float(top);
+  t.mul = fine ? 127.f / t.top : 0.f;
+  t.scale = fine ? t.top * t.inv / 127.f : top == 0 ? 0.f : __builtin_nanf("");
+  return t;
+}
+
+// Eight tokens of a row to int8 (top: of these tokens, in LDS).
+__device__ __forceinline__ uint2 round8(const float (&f)[8], const float (&mul)[8], const float* top) {
+  float u[8], d[8], far = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    u[e] = __builtin_fmaf(f[e], mul[e], MAGIC);
+    d[e] = __builtin_fmaf(f[e], mul[e], MAGIC - u[e]);
+    far = __builtin_fmaxf(far, __builtin_fabsf(d[e]));
+  }
+  if (far > 0.49998f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (__builtin_fabsf(d[e]) > 0.49998f) u[e] = settle(f[e], top[e], u[e] - MAGIC, d[e]) + MAGIC;
+  }
+  uint32_t q[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 1]), __float_as_uint(u[4 * e]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 3]), __float_as_uint(u[4 * e + 2]), 0x04000c0cu);
+    q[e] = lo | hi;
+  }
+  return make_uint2(q[0], q[1]);
+}
+// Eight tokens of a row to memory; only the first `tail` of the piece that ends behind the last token.
+__device__ __forceinline__ void store8(_Float16* p, half8 v, bool whole, int tail) {
+  if (whole) *(half8*)p = v;
+  else
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < tail) p[e] = v[e];
+}
+__device__ __forceinline__ void store8(int8_t* p, uint2 q, bool whole, int tail) {
+  if (whole) *(uint2*)p = q;
+  else
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (e < tail) p[e] = (int8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+}
+
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
@@ -137,13 +190,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
   };
   auto store_half = [&](_Float16* to, int i, half8 v) {
     const int k = r0 + i * RPP;
-    if (k >= g.K || !live) return;
-    _Float16* p = (_Float16*)((char*)(to + (size_t)(i * RPP) * g.ld + m0) + lane_at);
-    if (whole) *(half8*)p = v;
-    else
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < tail) p[e] = v[e];
+    if (k < g.K && live) store8((_Float16*)((char*)(to + (size_t)(i * RPP) * g.ld + m0) + lane_at), v, whole, tail);
   };
 
   // Norm: sums of squares and the largest |g|, as fp32; an infinity or NaN among the h of a token shows in its sum, one
@@ -236,15 +283,11 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
       if constexpr (NORM) s += s_sum[w][tid];
       t = max(t, s_top[w][tid]);
     }
-    float inv = 1.f;
-    if constexpr (NORM) inv = 1.f / sqrtf(s / (float)g.K + g.eps);
-    const bool fine = t != 0 && t < INF_BITS;
-    const float big = __uint_as_float(t);
-    s_inv[tid] = inv;
-    s_max[tid] = big;
-    s_mul[tid] = fine ? 127.f / big : 0.f;
-    if (g.scale && m0 + tid < g.M)
-      g.scale[m0 + tid] = fine ? big * inv / 127.f : t == 0 ? 0.f : __builtin_nanf("");
+    const Token x = finish_token<NORM>(s, t, g);
+    s_inv[tid] = x.inv;
+    s_max[tid] = x.top;
+    s_mul[tid] = x.mul;
+    if (g.scale && m0 + tid < g.M) g.scale[m0 + tid] = x.scale;
   }
   __syncthreads();
   float inv[8], mul[8];
@@ -258,34 +301,12 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
     store_half(g.Y, i, y);
   };
   auto store_q = [&](int i, half8 x, float gm) {
-    float f[8], u[8], d[8], far = 0.f;
+    float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      f[e] = NORM ? (float)x[e] * gm : (float)x[e];
-      u[e] = __builtin_fmaf(f[e], mul[e], MAGIC);
-      d[e] = __builtin_fmaf(f[e], mul[e], MAGIC - u[e]);
-      far = __builtin_fmaxf(far, __builtin_fabsf(d[e]));
-    }
-    if (far > 0.49998f) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (__builtin_fabsf(d[e]) > 0.49998f) u[e] = settle(f[e], s_max[c * 8 + e], u[e] - MAGIC, d[e]) + MAGIC;
-    }
-    uint32_t q[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 1]), __float_as_uint(u[4 * e]), 0x0c0c0400u);
-      const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(u[4 * e + 3]), __float_as_uint(u[4 * e + 2]), 0x04000c0cu);
-      q[e] = lo | hi;
-    }
+    for (int e = 0; e < 8; ++e) f[e] = NORM ? (float)x[e] * gm : (float)x[e];
+    const uint2 q = round8(f, mul, s_max + c * 8);
     const int k = r0 + i * RPP;
-    if (k >= g.K || !live) return;
-    int8_t* p = g.Q + (size_t)(i * RPP) * g.ldq + m0 + ((uint64_t)r0 * g.ldq + c * 8);
-    if (whole) *(uint2*)p = make_uint2(q[0], q[1]);
-    else
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < tail) p[e] = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
+    if (k < g.K && live) store8(g.Q + (size_t)(i * RPP) * g.ldq + m0 + ((uint64_t)r0 * g.ldq + c * 8), q, whole, tail);
   };
   auto second_pass = [&](int i0) {
     if (NORM && g.Y) {
@@ -327,6 +348,235 @@ hipError_t run_norm(const NormArgs& g, hipStream_t stream) {
   return launch_kernel(norm_kernel<NORM, TOK, NT, NCH, NL>, dim3(8 * per * (64 / TOK)), dim3(NT), stream, g);
 }
 
+// ---- long tokens in slices of their rows ----------------------------------------------------------
+// A workgroup that owns whole tokens reads and writes narrow pieces of rows (64 and 32 bytes, of lines of 128).  With many rows
+// three launches on 128 tokens x one slice of the rows are faster, every access whole lines: sums of the slices (and H), sums of
+// the tokens, outputs.  No memory beyond the outputs is used: between the launches the sums of a slice, 8 bytes per token, lie in
+// the first rows of that slice of Q (8 rows of bytes; of Y 4 rows of halves without Q), which the last launch reads before it
+// writes them.  us, one launch / three (residual, int8 output, from HBM): 4096
+// rows, 1024 tokens 26 / 20, 4096 tokens 49 / 42, 8192 tokens 79 / 68, with both outputs 105 / 85; 8192 rows, 1024 tokens 52 / 28,
+// 8192 tokens 167 / 128; 2048 rows, 4096 tokens 25 / 27, 8192 tokens 41 / 43; 4096 rows, 512 tokens 18 / 19, without a
+// residual, 8192 tokens 39 / 47.
+constexpr int SL_TOK = 128, SL_NT = 256, SL_RPP = SL_NT / (SL_TOK / 8), SL_CH = 8;      // 16 rows at a time, 8 times
+
+__device__ __forceinline__ int slice_row(const NormArgs& g, int s, int n) { return (int)((int64_t)g.K * s / n); }
+
+__device__ __forceinline__ uint2 get_sums(const NormArgs& g, int k, int m) {
+  uint32_t w[2] = {0u, 0u};
+  if (g.Q) {
+    uint32_t b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = ((const uint8_t*)g.Q)[(size_t)(k + j) * g.ldq + m];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j >> 2] |= b[j] << (8 * (j & 3));
+  } else {
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = ((const uint16_t*)g.Y)[(size_t)(k + j) * g.ld + m];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j >> 1] |= b[j] << (16 * (j & 1));
+  }
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void put_sums(const NormArgs& g, int k, int m, uint2 v) {
+  if (g.Q) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ((uint8_t*)g.Q)[(size_t)(k + j) * g.ldq + m] = (uint8_t)((j < 4 ? v.x : v.y) >> (8 * (j & 3)));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ((uint16_t*)g.Y)[(size_t)(k + j) * g.ld + m] = (uint16_t)((j < 2 ? v.x : v.y) >> (16 * (j & 1)));
+  }
+}
+
+// What both kernels over slices know of their place.
+struct SliceLane {
+  int s, k0, k1, m0, m, c, r0, tail;
+  bool live, whole;
+  size_t at;
+  __device__ __forceinline__ SliceLane(const NormArgs& g, int n) {
+    const int bands = (g.M + SL_TOK - 1) / SL_TOK;
+    s = (int)blockIdx.x / bands;
+    m0 = ((int)blockIdx.x - s * bands) * SL_TOK;
+    k0 = slice_row(g, s, n);
+    k1 = slice_row(g, s + 1, n);
+    c = threadIdx.x % (SL_TOK / 8);
+    r0 = threadIdx.x / (SL_TOK / 8);
+    m = m0 + c * 8;
+    live = m < g.M;
+    whole = m + 8 <= g.M;
+    tail = g.M & 7;
+    at = (size_t)(live ? m : m0);
+  }
+  __device__ __forceinline__ int row(int i) const { return k0 + r0 + i * SL_RPP; }
+  __device__ __forceinline__ half8 load(const _Float16* from, const NormArgs& g, int i) const {
+    return *(const half8*)(from + (size_t)min(row(i), k1 - 1) * g.ld + at);
+  }
+};
+
+__global__ __launch_bounds__(SL_NT) void norm_slices_kernel(NormArgs g, int n) {
+  __shared__ float s_sum[4][SL_TOK], s_top[4][SL_TOK];
+  const SliceLane a(g, n);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  half8 h[SL_CH];
+  _Float16 gam[SL_CH];
+#pragma unroll
+  for (int i = 0; i < SL_CH; ++i) h[i] = a.load(g.X, g, i);
+#pragma unroll
+  for (int i = 0; i < SL_CH; ++i) gam[i] = (_Float16)1.f;
+  if (g.gamma) {
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) gam[i] = g.gamma[min(a.row(i), a.k1 - 1)];
+  }
+  if (g.R) {
+    half8 r[SL_CH];
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) r[i] = a.load(g.R, g, i);
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) h[i] += r[i];
+  }
+  if (g.H) {
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i)
+      if (a.row(i) < a.k1 && a.live) store8(g.H + (size_t)a.row(i) * g.ld + a.m, h[i], a.whole, a.tail);
+  }
+  float sum[8], top[8], worst = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { sum[e] = 0.f; top[e] = 0.f; }
+#pragma unroll
+  for (int i = 0; i < SL_CH; ++i) {
+    if (a.row(i) >= a.k1) h[i] = half8{0, 0, 0, 0, 0, 0, 0, 0};
+    const float gm = (float)gam[i];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float f = (float)h[i][e];
+      sum[e] = __builtin_fmaf(f, f, sum[e]);
+      top[e] = __builtin_fmaxf(top[e], __builtin_fabsf(f * gm));
+    }
+    worst = __builtin_fmaf(gm, 0.f, worst);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] += worst;
+  halve(sum, [](float x, float y) { return x + y; });
+  halve(top, [](float x, float y) { return __builtin_fmaxf(x, y); });
+  const int tok = a.c * 8 + 2 * (lane >> 4 & 1) + 4 * (lane >> 5);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    s_sum[wave][tok + e] = sum[e];
+    s_top[wave][tok + e] = top[e];
+  }
+  __syncthreads();
+  if (tid < SL_TOK && a.m0 + tid < g.M) {
+    const float x = s_sum[0][tid] + s_sum[1][tid] + s_sum[2][tid] + s_sum[3][tid];
+    float t = s_top[0][tid];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) t = __builtin_fmaxf(t, s_top[w][tid]);
+    put_sums(g, a.k0, a.m0 + tid, make_uint2(__float_as_uint(x), x < __builtin_inff() ? __float_as_uint(t) : INF_BITS));
+  }
+}
+
+// 16 tokens, 16 groups of threads on the slices by turns: up to 32 slices (4096 rows) in one round trip.
+constexpr int TK_TOK = 16, TK_GRP = 16;
+__global__ __launch_bounds__(TK_TOK * TK_GRP) void norm_tokens_kernel(NormArgs g, int n) {
+  __shared__ float s_sum[TK_GRP][TK_TOK];
+  __shared__ uint32_t s_top[TK_GRP][TK_TOK];
+  __shared__ uint2 s_out[TK_TOK];
+  const int tok = threadIdx.x % TK_TOK, grp = threadIdx.x / TK_TOK, m = (int)blockIdx.x * TK_TOK + tok;
+  float sum = 0.f;
+  uint32_t top = 0;
+  if (m < g.M)
+    for (int s = grp; s < n; s += 2 * TK_GRP) {
+      const uint2 v = get_sums(g, slice_row(g, s, n), m);
+      const uint2 w = get_sums(g, slice_row(g, min(s + TK_GRP, n - 1), n), m);
+      sum += __uint_as_float(v.x);
+      top = max(top, v.y);
+      if (s + TK_GRP < n) {
+        sum += __uint_as_float(w.x);
+        top = max(top, w.y);
+      }
+    }
+  s_sum[grp][tok] = sum;
+  s_top[grp][tok] = top;
+  __syncthreads();
+  if (grp == 0) {
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < TK_GRP; ++w) {
+      sum += s_sum[w][tok];
+      top = max(top, s_top[w][tok]);
+    }
+    const Token t = finish_token<true>(sum, top, g);
+    if (g.scale && m < g.M) g.scale[m] = t.scale;
+    s_out[tok] = make_uint2(__float_as_uint(t.inv), top);
+  }
+  __syncthreads();
+  if (m < g.M)
+    for (int s = grp; s < n; s += TK_GRP) put_sums(g, slice_row(g, s, n), m, s_out[tok]);
+}
+
+__global__ __launch_bounds__(SL_NT) void norm_outputs_kernel(NormArgs g, int n) {
+  __shared__ __attribute__((aligned(16))) float s_inv[SL_TOK], s_mul[SL_TOK], s_max[SL_TOK];
+  const SliceLane a(g, n);
+  const int tid = threadIdx.x;
+  half8 h[SL_CH];
+  _Float16 gam[SL_CH];
+  const _Float16* from = g.H ? g.H : g.X;
+#pragma unroll
+  for (int i = 0; i < SL_CH; ++i) h[i] = a.load(from, g, i);
+#pragma unroll
+  for (int i = 0; i < SL_CH; ++i) gam[i] = (_Float16)1.f;
+  if (g.gamma) {
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) gam[i] = g.gamma[min(a.row(i), a.k1 - 1)];
+  }
+  if (g.R && !g.H) {
+    half8 r[SL_CH];
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) r[i] = a.load(g.R, g, i);
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) h[i] += r[i];
+  }
+  if (tid < SL_TOK) {
+    const uint2 v = a.m0 + tid < g.M ? get_sums(g, a.k0, a.m0 + tid) : make_uint2(0u, 0u);
+    const float big = __uint_as_float(v.y);
+    s_inv[tid] = __uint_as_float(v.x);
+    s_max[tid] = big;
+    s_mul[tid] = v.y != 0 && v.y < INF_BITS ? 127.f / big : 0.f;
+  }
+  __syncthreads();                       // every sum of the slice has been read; its rows are written now
+  float inv[8], mul[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { inv[e] = s_inv[a.c * 8 + e]; mul[e] = s_mul[a.c * 8 + e]; }
+  if (!a.live) return;
+  if (g.Y) {
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) {
+      half8 y;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = (_Float16)((float)h[i][e] * (float)gam[i] * inv[e]);
+      if (a.row(i) < a.k1) store8(g.Y + (size_t)a.row(i) * g.ld + a.m, y, a.whole, a.tail);
+    }
+  }
+  if (g.Q) {
+#pragma unroll
+    for (int i = 0; i < SL_CH; ++i) {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (float)h[i][e] * (float)gam[i];
+      const uint2 q = round8(f, mul, s_max + a.c * 8);
+      if (a.row(i) < a.k1) store8(g.Q + (size_t)a.row(i) * g.ldq + a.m, q, a.whole, a.tail);
+    }
+  }
+}
+
+// n slices of at most 128 and at least 8 rows.
+hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
+  const unsigned bands = (unsigned)(((int64_t)g.M + SL_TOK - 1) / SL_TOK);
+  hipError_t e = launch_kernel(norm_slices_kernel, dim3(bands * n), dim3(SL_NT), stream, g, n);
+  if (e == hipSuccess) e = launch_kernel(norm_tokens_kernel, dim3((unsigned)(((int64_t)g.M + TK_TOK - 1) / TK_TOK)), dim3(TK_TOK * TK_GRP), stream, g, n);
+  if (e == hipSuccess) e = launch_kernel(norm_outputs_kernel, dim3(bands * n), dim3(SL_NT), stream, g, n);
+  return e;
+}
+
 #ifndef TUNE
 // Tokens per workgroup: 8 while that is at most one workgroup per CU (few rows of a token per lane and every CU at
 // work), 16 up to two, then 32, whose pieces of a row are half a line of memory; above 16384 whole lines.
@@ -337,6 +587,7 @@ hipError_t run_norm(const NormArgs& g, hipStream_t stream) {
 template <bool NORM>
 static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   const int K = g.K;
+  if (NORM && g.R && K > 2048 && (int64_t)g.M * K >= 3 << 20) return run_norm_slices(g, (K + SL_CH * SL_RPP - 1) / (SL_CH * SL_RPP), stream);
   if (g.M <= 2048 && K <= 8192) {
     if (K <= 1024) return run_norm<NORM, 8, 512, 2>(g, stream);
     if (K <= 2048) return run_norm<NORM, 8, 512, 4>(g, stream);

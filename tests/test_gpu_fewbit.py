@@ -81,6 +81,7 @@ def test_norm_and_quantiser_of_many_tokens(M, K):
     X, R = acts(M + K, M, K), acts(M + K + 1, M, K, 3.0)
     X[M - 2, K // 2] = np.inf
     _check_norm(X, R, None, 1e-5, i8=True, f16=True)
+    _check_norm(X, None, None, 1e-5, i8=True, f16=True)
     q, scale = ofb.quant_i8(X)
     Xd, ldq = dev_km(X, up(M, 8)), up(M, 16)
     Q, s = torch.full((K, ldq), 99, dtype=torch.int8, device="cuda"), torch.zeros((M,), device="cuda")
@@ -88,6 +89,36 @@ def test_norm_and_quantiser_of_many_tokens(M, K):
     assert np.array_equal(Q.cpu().numpy()[:, :M].T, q) and (Q[:, M:] == 99).all()
     s = s.cpu().numpy()
     assert np.array_equal(np.isnan(s), np.isnan(scale)) and (np.abs(np.nan_to_num(s - scale)) <= 2.0 ** -23 * np.nan_to_num(scale)).all()
+
+
+@pytest.mark.parametrize("M,K", [(1537, 2049), (1001, 3333), (768, 4096), (400, 8200)])
+def test_norm_of_long_tokens_in_slices(M, K):
+    """With a residual and many rows the work is cut along the rows: every combination of outputs, in place, infinities."""
+    print(f"slices M={M} K={K}", flush=True)
+    X, R = acts(M + K, M, K), acts(M + K + 1, M, K, 3.0)
+    gamma = (1 + 0.3 * np.random.default_rng(K).standard_normal(K)).astype(np.float16)
+    _check_norm(X, R, gamma, 1e-5, i8=True, f16=True)
+    _check_norm(X, R, gamma, 1e-5, i8=False, f16=True, alias="X", ld=up(M, 8) + 16)
+    _check_norm(X, R, None, 1e-5, i8=True, f16=False, alias="R", ldq=up(M, 16) + 32)
+    _check_norm(X, R, gamma, 1e-5, i8=True, f16=False, H=False)
+    _check_norm(X, R, None, 1e-5, i8=False, f16=True, H=False)
+    X[3, 7], X[20, K - 1], R[33, 0], X[M - 1, 130] = np.inf, np.nan, -np.inf, np.nan
+    X[40, 5] = R[40, 5] = 60000.0
+    _check_norm(X, R, gamma, 1e-5, i8=True, f16=True)
+    gamma[K - 2] = np.nan                                 # every token
+    _, _, Q, s = _norm(X, R, gamma, 1e-5, i8=True, f16=False)
+    assert np.isnan(s[:M]).all() and not Q[:, :M].any()
+
+
+@pytest.mark.parametrize("K", [5, 1500, 5000])
+def test_norm_with_a_gamma_that_is_not_finite(K):
+    M = 40
+    X = acts(7, M, K)
+    for bad in (np.nan, np.inf):
+        gamma = np.ones(K, np.float16)
+        gamma[K // 2] = bad
+        _, _, Q, s = _norm(X, None, gamma, 1e-5, i8=True, f16=False)
+        assert np.isnan(s[:M]).all() and not Q[:, :M].any()
 
 
 @pytest.mark.parametrize("alias", ["X", "R"])
