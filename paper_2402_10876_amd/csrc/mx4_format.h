@@ -32,10 +32,12 @@ inline uint8_t mx4_scale_of(uint16_t top) {
   memcpy(&u, &f, 4);
   return (uint8_t)((u >> 23) - 2);      // (the exponent's field is 127 + floor(log2))
 }
-// Code of an fp16 value in a block with this scale byte: the number of midpoints below it, a midpoint itself counting
+// What a block with this scale byte multiplies its values with.
+inline float mx4_factor(uint8_t scale) { return mx4_bits_to_float((uint32_t)(254 - scale) << 23); }
+// Code of an fp16 value in a block with this factor: the number of midpoints below it, a midpoint itself counting
 // where the code above is the even one.
-inline uint8_t mx4_code(uint16_t h, uint8_t scale) {
-  const float t = mx4_magnitude(h) * mx4_bits_to_float((uint32_t)(254 - scale) << 23);
+inline uint8_t mx4_code(uint16_t h, float factor) {
+  const float t = mx4_magnitude(h) * factor;
   const int c = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) + (t > 2.5f) + (t >= 3.5f) + (t > 5.f);
   return (uint8_t)(c | (h >> 15 << 3));
 }

@@ -220,6 +220,9 @@ tw_status pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* tile_
   return TW_ERR_ALLOC;
 }
 
+static void build_mx4_lists(tw_handle_s* h);
+static void build_mx4_values(tw_handle_s* h);
+
 // Microscaled 4-bit weights: kept columns are those with any mask bit, cut into tiles of G; a tile keeps a block of 32 rows
 // whole if the mask keeps anything of it there.  `values` are what the blocks stand for (fp16).
 tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_s* h) try {
@@ -245,6 +248,7 @@ tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, in
   h->values.resize((size_t)h->sum_kw);
   uint16_t top[128];
   uint8_t scale[128];
+  float factor[128];
   for (int t = 0; t < n_tiles; ++t) {
     const int w = h->tile_col_off[t + 1] - h->tile_col_off[t];
     const int32_t* cols = h->col_idx.data() + h->tile_col_off[t];
@@ -263,26 +267,28 @@ tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, in
       for (int c = 0; c < w; ++c) {
         if (top[c] >= 0x7c00) return TW_ERR_ARG;
         scale[c] = mx4_scale_of(top[c]);
+        factor[c] = mx4_factor(scale[c]);
       }
       for (int k = 0; k < n; ++k)
         for (int c = 0; c < w; ++c) {
           uint16_t& x = v[(size_t)k * w + c];
-          x = value[scale[c]][mx4_code(x, scale[c])];
+          x = value[scale[c]][mx4_code(x, factor[c])];
         }
       v += (size_t)n * w;
       i += n;
     }
   }
-  build_device_image(h);
+  build_mx4_lists(h);
+  build_mx4_values(h);
   return TW_OK;
 } catch (const std::bad_alloc&) {
   return TW_ERR_ALLOC;
 }
 
-// The image of a microscaled 4-bit weight from its logical form (layout at Mx4Image).
-static void build_mx4_image(tw_handle_s* h) {
+// The image of a microscaled 4-bit weight from its logical form (layout at Mx4Image): the lists, then the values.
+static void build_mx4_lists(tw_handle_s* h) {
   Mx4Image& d = h->mx4;
-  const int G = h->G, GB = G / 32;
+  const int G = h->G;
   std::vector<int32_t> members = h->member_n;
   if (members.empty()) members.assign(1, h->N);
   std::vector<uint8_t> is_kept(h->N, 0);
@@ -334,11 +340,19 @@ static void build_mx4_image(tw_handle_s* h) {
       for (int c = h->tile_col_off[t]; c < h->tile_col_off[t + 1]; ++c) d.col_idx[at * G + c - h->tile_col_off[t]] = h->col_idx[c];
     }
   }
-  d.vals.assign((size_t)step * GB * 1024, 0);
-  d.scales.assign((size_t)step * GB * 64, (uint8_t)MX4_ONE);
-  int64_t s0 = 0;
+}
+
+static void build_mx4_values(tw_handle_s* h) {
+  Mx4Image& d = h->mx4;
+  const int GB = h->G / 32;
+  int64_t steps = 0, s0 = 0;
+  for (const Mx4Tile& r : d.tiles) steps += r.steps;
+  d.vals.assign((size_t)steps * GB * 1024, 0);
+  d.scales.assign((size_t)steps * GB * 64, (uint8_t)MX4_ONE);
   uint16_t top[128];
-  for (int tl = 0; tl < h->n_tiles; ++tl) {    // values (the tiles that fill up have no steps)
+  float factor[128];
+  uint8_t code[MX4_BLOCK][128];
+  for (int tl = 0; tl < h->n_tiles; ++tl) {    // (the tiles that fill up have no steps)
     const int w = h->tile_col_off[tl + 1] - h->tile_col_off[tl];
     const uint16_t* v = h->values.data() + h->val_off[tl];
     int b = 0;
@@ -349,11 +363,16 @@ static void build_mx4_image(tw_handle_s* h) {
       for (int k = 0; k < n; ++k)
         for (int c = 0; c < w; ++c) top[c] = std::max(top[c], (uint16_t)(v[(size_t)k * w + c] & 0x7fff));
       for (int c = 0; c < w; ++c) {
-        const int lane = c % 32 + 32 * (b % 2), nb = c / 32;
         const uint8_t sc = mx4_scale_of(top[c]);
-        d.scales[((size_t)s * 64 + lane) * GB + nb] = sc;
-        uint8_t* out = d.vals.data() + (((size_t)s * GB + nb) * 64 + lane) * 16;
-        for (int k = 0; k < n; ++k) out[k / 2] |= (uint8_t)(mx4_code(v[(size_t)k * w + c], sc) << (4 * (k % 2)));
+        d.scales[((size_t)s * 64 + c % 32 + 32 * (b % 2)) * GB + c / 32] = sc;
+        factor[c] = mx4_factor(sc);
+      }
+      for (int k = 0; k < n; ++k)
+        for (int c = 0; c < w; ++c) code[k][c] = mx4_code(v[(size_t)k * w + c], factor[c]);
+      for (int k = n; k < MX4_BLOCK; ++k) std::fill(code[k], code[k] + w, (uint8_t)0);
+      for (int c = 0; c < w; ++c) {
+        uint8_t* out = d.vals.data() + (((size_t)s * GB + c / 32) * 64 + c % 32 + 32 * (b % 2)) * 16;
+        for (int k = 0; k < 16; ++k) out[k] = (uint8_t)(code[2 * k][c] | code[2 * k + 1][c] << 4);
       }
       v += (size_t)n * w;
       i += n;
@@ -445,6 +464,14 @@ tw_status concat_host(const tw_handle_s* const* parts, int n, tw_handle_s* h) tr
   for (int32_t r : h->ew_row) used[r] = 1;
   h->k_union = 0;
   for (int k = 0; k < h->K; ++k) h->k_union += used[k];
+  if (h->dtype == TW_DTYPE_MX4) {              // the members' blocks as they are
+    build_mx4_lists(h);
+    for (int i = 0; i < n; ++i) {
+      h->mx4.vals.insert(h->mx4.vals.end(), parts[i]->mx4.vals.begin(), parts[i]->mx4.vals.end());
+      h->mx4.scales.insert(h->mx4.scales.end(), parts[i]->mx4.scales.begin(), parts[i]->mx4.scales.end());
+    }
+    return TW_OK;
+  }
   build_device_image(h);
   return TW_OK;
 } catch (const std::bad_alloc&) {
@@ -471,7 +498,6 @@ tw_status concat_host(const tw_handle_s* const* parts, int n, tw_handle_s* h) tr
 //      16-bit half selected by its ABID field, 2 bits per stored element).
 // ---------------------------------------------------------------------------
 void build_device_image(tw_handle_s* h) {
-  if (h->dtype == TW_DTYPE_MX4) { build_mx4_image(h); return; }
   build_device_lists(h);
   build_device_values(h);
 }

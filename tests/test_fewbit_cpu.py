@@ -125,9 +125,9 @@ int main() {
   for (int h = 0; h < 0x7c00; ++h)                  // every finite magnitude: value of the code of the value
     for (int up = 0; up < 3; ++up) {
       const int top = std::min(h + 1024 * up, 0x7bff);
-      const uint8_t s = twg::mx4_scale_of((uint16_t)top), c = twg::mx4_code((uint16_t)h, s);
+      const uint8_t s = twg::mx4_scale_of((uint16_t)top), c = twg::mx4_code((uint16_t)h, twg::mx4_factor(s));
       const uint16_t v = twg::mx4_value(c, s);
-      if (twg::mx4_code(v, s) != c || (up == 0 && twg::mx4_scale_of(v) != s)) ++fails;
+      if (twg::mx4_code(v, twg::mx4_factor(s)) != c || (up == 0 && twg::mx4_scale_of(v) != s)) ++fails;
     }
   for (int it = 0; it < 40; ++it) {
     const int K = 1 + rng() % 150, N = 1 + rng() % 300, G = rng() % 2 ? 64 : 128;
