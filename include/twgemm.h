@@ -368,7 +368,8 @@ tw_status tw_conv_gemm_i8(const void* X_dev, tw_conv_t binding, void* C_dev, int
  * Common to the calls below: activations are K x M (token m of row k at X[k*ld + m], TW_LAYOUT_KM), device memory, 16-byte
  * aligned; the scales of tw_rmsnorm / tw_quant_i8 / tw_gemm_i8_scaled are 4-byte aligned.  Columns M .. ld-1 are never
  * written; they may be read (whatever they hold) and have to be readable (row-major input: values K .. ldx-1 of a row).  M <= 2^27 (the 4-bit calls: ldq <= 2^27) and
- * K <= 131071, else TW_ERR_UNSUPPORTED.  Asynchronous on `stream`, allocate nothing, keep no state between calls.
+ * K <= 131071, else TW_ERR_UNSUPPORTED.  Outputs must not overlap anything else (H_dev of tw_rmsnorm: see there); the address of
+ * another operand as an output is TW_ERR_ARG.  Asynchronous on `stream`, allocate nothing, keep no state between calls.
  * Unlike elsewhere in this library an infinity or NaN is an allowed input of the norm and the quantisers: it marks its token
  * (its block of a token) as said there and reaches no other.
  *
@@ -383,13 +384,14 @@ tw_status tw_conv_gemm_i8(const void* X_dev, tw_conv_t binding, void* C_dev, int
  *   Y_dev     fp16 output, same ld, or NULL
  *   Q_dev, scale_dev  int8 K x M (ldq >= M, multiple of 16: the operand of tw_gemm_i8 / tw_gemm_i8_scaled) and M floats; or
  *             both NULL.  One of Y_dev and Q_dev is needed.
- *   Outputs must not overlap anything else.  Errors: TW_ERR_ARG, TW_ERR_UNSUPPORTED, TW_ERR_HIP.
+ *   Errors: TW_ERR_ARG, TW_ERR_UNSUPPORTED, TW_ERR_HIP.
  * tw_quant_i8 - the int8 output alone, of activations as they are: scale[m] = max_k|x| / 127, Q as above.
  *
  * tw_gemm_i8_scaled - tw_gemm_i8 whose output is fp16 in real units:
  *     C[n][m] = fp16( fp32(sum) * (a_scale[m] * w_scale[n]) ),  every step one rounding
  *   a_scale_dev M floats (of the tokens), w_scale_dev N floats (of the weight's columns); C_dev fp16, ldc >= M, multiple of
- *   8; pruned columns are +0.  A, M, lda, the handle and the errors as tw_gemm_i8.
+ *   8; pruned columns are +0.  A, M, lda, the handle and the errors as tw_gemm_i8; TW_ERR_STATE also on another
+ *   device than the handle's.
  *
  * Microscaled 4-bit floating point (TW_DTYPE_MX4).  32 consecutive rows of a column (of a token) are a block: 32 codes
  * of e2m1 (sign, 2 bits exponent, 1 bit mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one scale byte s, a factor 2^(s-127).

@@ -769,8 +769,12 @@ tw_status tw_gemm_i8_scaled(const void* A, int M, int lda, tw_handle_t h, const 
   if (!aligned16(A) || !aligned16(C) || lda % 16 || ldc % 8 || lda < M || ldc < M) return TW_ERR_ARG;
   if (((uintptr_t)a_scale & 3) || ((uintptr_t)w_scale & 3) || h->dtype != TW_DTYPE_I8) return TW_ERR_ARG;
   if (!h->img.blob) return TW_ERR_STATE;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
+  if (dev != h->img.device) return TW_ERR_STATE;
   if (h->G == 32 || h->K > 131071) return TW_ERR_UNSUPPORTED;
   if ((unsigned long long)h->K * (unsigned long long)lda >= (1ull << 32)) return TW_ERR_UNSUPPORTED;
+  if (C == A || C == (const void*)a_scale || C == (const void*)w_scale) return TW_ERR_ARG;
   return gemm_i8_launch(A, M, lda, h, C, ldc, 2, 0.f, stream, nullptr, a_scale, w_scale);
 }
 
@@ -813,6 +817,14 @@ tw_status tw_rmsnorm(const void* X, const void* R, const void* gamma, float eps,
   if (!aligned16(X) || !aligned16(R) || !aligned16(H) || !aligned16(Y) || !aligned16(Q)) return TW_ERR_ARG;
   if (((uintptr_t)gamma & 1) || ((uintptr_t)scale & 3) || (Q && (ldq < M || ldq % 16))) return TW_ERR_ARG;
   if (M > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  const void* in[4] = {X, R, gamma, H};                      // (H may be X or R)
+  const void* out[3] = {Y, Q, scale};
+  for (int o = 0; o < 3; ++o) {
+    for (const void* i : in)
+      if (out[o] && out[o] == i) return TW_ERR_ARG;
+    if (out[o] && out[o] == out[(o + 1) % 3]) return TW_ERR_ARG;
+  }
+  if (gamma && gamma == H) return TW_ERR_ARG;
   const twg::NormArgs g{(const _Float16*)X, (const _Float16*)R, (const _Float16*)gamma, (_Float16*)H, (_Float16*)Y, (int8_t*)Q,
                         scale, M, K, ld, ldq, eps};
   return twg::launch_norm(true, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
@@ -822,6 +834,7 @@ tw_status tw_quant_i8(const void* X, int M, int K, int ldx, void* Q, int ldq, fl
   if (!X || !Q || !scale || M < 1 || K < 1 || ldx < M || ldx % 8 || ldq < M || ldq % 16) return TW_ERR_ARG;
   if (!aligned16(X) || !aligned16(Q) || ((uintptr_t)scale & 3)) return TW_ERR_ARG;
   if (M > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  if (X == Q || X == (const void*)scale || Q == (void*)scale) return TW_ERR_ARG;
   const twg::NormArgs g{(const _Float16*)X, nullptr, nullptr, nullptr, nullptr, (int8_t*)Q, scale, M, K, ldx, ldq, 0.f};
   return twg::launch_norm(false, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
 }
@@ -832,6 +845,7 @@ tw_status tw_quant_mx4(const void* X, int M, int K, int ldx, int layout, void* Q
   if (ldx < (layout == TW_LAYOUT_KM ? M : K)) return TW_ERR_ARG;
   if (!aligned16(X) || !aligned16(Q) || !aligned16(S)) return TW_ERR_ARG;
   if (ldq > MOST_TOKENS || K > 131071) return TW_ERR_UNSUPPORTED;
+  if (X == Q || X == S || Q == S) return TW_ERR_ARG;
   const twg::QuantMx4Args g{(const _Float16*)X, (uint8_t*)Q, (uint8_t*)S, M, K, ldx, ldq};
   return twg::launch_quant_mx4(layout == TW_LAYOUT_KM, g, (hipStream_t)stream) == hipSuccess ? TW_OK : TW_ERR_HIP;
 }
@@ -867,6 +881,7 @@ static tw_status gemm_mx4_launch(const void* Q, const void* S, int M, int ldq, c
   if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
   if (dev != h->img.device) return TW_ERR_STATE;
   if (ldq > MOST_TOKENS) return TW_ERR_UNSUPPORTED;
+  if (C == Q || C == S || C == (const void*)offsets) return TW_ERR_ARG;
   const twg::Mx4Image& d = h->mx4;
   const char* p = (const char*)h->img.blob;
   twg::GemmMx4Args g{};

@@ -8,8 +8,9 @@
 // u, wrong only within 127 * 2^-24 of a half; where the distance to n is more than 0.49998 the side is settled in 64 bits
 // (254 g against (2n +- 1) max|g|, both exact).  Sums of squares are fp32 (at most 32 terms a lane, then a tree).
 //
-// Bound by memory: 2 bytes in per value (4 with a residual), 1 to 5 out.  One workgroup owns 32 tokens and all K rows and
-// keeps its values in registers between the two passes, up to 16 rows a lane; longer columns are read again, from L2.
+// Bound by memory: 2 bytes in per value (4 with a residual), 1 to 5 out.  One workgroup owns 8 to 64 tokens and all K rows and
+// keeps its values in registers (and LDS) between the two passes, up to 16 rows a lane; longer columns are read again, from L2.
+// Many long tokens with a residual go in slices of their rows (below).
 #include <type_traits>
 
 #include "device_common.h"
@@ -580,10 +581,10 @@ hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
 #ifndef TUNE
 // Tokens per workgroup: 8 while that is at most one workgroup per CU (few rows of a token per lane and every CU at
 // work), 16 up to two, then 32, whose pieces of a row are half a line of memory; above 16384 whole lines.
-// Rows in registers as far as they fit, fewer lanes where they would have nothing to do.  us with 8 / 16 / 32 tokens (residual, int8
-// output, same buffers): 768 rows, 2048 tokens 6.5 / 7.0 / 8.1, 4096 tokens 8.8 / 8.1 / 9.3; 4096 rows, 16 tokens 6.4 / 9.5 / 13,
-// 1024 tokens 19 / 22 / 29, 4096 tokens 57 / 48 / 59, 8192 tokens 106 / 99 / 77; 1024 rows, 8192 tokens - / 24 / 20;
-// 4096 rows, 16384 tokens, 32 / 64 160 / 143, 8192 tokens 77 / 93.
+// Rows in registers as far as they fit, fewer lanes where they would have nothing to do.  us with 8 / 16 / 32 / 64 tokens, int8
+// output, from HBM, with a residual: 768 rows, 2048 tokens 6.8 / 7.3 / 8.7, 4096 tokens 11.8 / 9.2 / 11.0; 1024 rows, 8192 tokens
+// 30 / 25 / 21 / 28; 4096 rows, 16 tokens 6.8 / 9.8 / 20, 512 tokens 17 / 23 / 35.  Without: 4096 rows, 1024 tokens 11.3 / 13.7 /
+// 20, 4096 tokens 28 / 23 / 32, 8192 tokens 51 / 46 / 42 / 47, 16384 tokens - / 91 / 90 / 77.
 template <bool NORM>
 static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   const int K = g.K;
@@ -602,7 +603,7 @@ static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   if (g.M < 1 << 25) {                   // (2^32 threads in a grid: none of 32 tokens beyond 2^27 - 1)
     if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
     if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
-    // half of them in LDS; with a residual the registers do not suffice (8192 x 4096: 77 us read again, 82 kept)
+    // half of the rows in LDS: the quantiser, 8192 x 4096, 36 us against 42 read again; the norm spills registers there
     if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);
     if (g.M <= 16384 - 64) return run_norm<NORM, 32, 1024, 0>(g, stream);
   }

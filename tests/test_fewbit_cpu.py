@@ -198,6 +198,17 @@ def test_norm_and_int8_quantiser_refuse():
         (6, None, 1), (6, P + 1, 1), (2, 131072, 3)])
 
 
+def test_an_output_that_is_another_operand_is_refused():
+    #       X  R     gamma  eps   M  K  ld H     Y      Q    ldq scale
+    good = [P, 2 * P, 3 * P, 1e-6, 9, 5, 16, 4 * P, 5 * P, 6 * P, 16, 7 * P]
+    for out in (8, 9, 11):
+        _each(tw.tw_rmsnorm, good, [(out, good[i], 1) for i in (0, 1, 2, 7, 8, 9, 11) if i != out])
+    _each(tw.tw_rmsnorm, good, [(7, good[2], 1)])
+    _each(tw.tw_quant_i8, [P, 9, 5, 16, 2 * P, 16, 3 * P], [(4, P, 1), (6, P, 1), (6, 2 * P, 1)])
+    for layout in (tw.LAYOUT_KM, tw.LAYOUT_MK):
+        _each(tw.tw_quant_mx4, [P, 9, 5, 16, layout, 2 * P, 3 * P, 16], [(5, P, 1), (6, P, 1), (6, 2 * P, 1)])
+
+
 def test_mx4_calls_refuse():
     _each(tw.tw_quant_mx4, [P, 9, 5, 16, tw.LAYOUT_KM, P, P, 16], [
         (0, None, 1), (0, P + 8, 1), (1, 0, 1), (2, 0, 1), (3, 8, 1), (3, 20, 1), (4, 2, 1), (5, None, 1), (5, P + 8, 1),
