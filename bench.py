@@ -26,8 +26,9 @@ Prints ONE JSON line: dense-equivalent TFLOP/s of the whole step, plus
                 BERT-large FFN sparsity sweep, the VGG-16 im2col GEMMs): time, our dense
                 kernel's time, binding roof and the fraction of it (outside the timed region);
   cpu_baseline  the fp64 oracle timed on the host cores.
-`--extra cube,imbalance,tew,i8,conv,options` adds opt-in sweeps (the 4096^3 sparsity sweep, uneven
-tiles, TEW, int8, convolutions without a materialised img2col matrix) under `extra`.
+`--extra cube,imbalance,tew,i8,fewbit,conv,options` adds opt-in sweeps (the 4096^3 sparsity sweep, uneven
+tiles, TEW, int8, layers in 8 and 4 bits between fp16 activations, convolutions without a materialised
+img2col matrix) under `extra`.
 `--calibrate` runs the calibration kernels alone (the command the rocprofv3 summary in
 profiles/ was taken with).
 """
@@ -199,12 +200,13 @@ def extra_rows(tw, wl, torch, dev, stream, skip_cfg, reps=24, sets=24):
 
 
 def extra_sweeps(tw, wl, torch, dev, stream, which, reps=24, sets=6):
-    """Opt-in measurements beyond the configured workloads (`--extra cube,imbalance,tew,i8,conv`; `options` is handled in main, on the step's own buffers):
+    """Opt-in measurements beyond the configured workloads (`--extra cube,imbalance,tew,i8,fewbit,conv`; `options` is handled in main, on the step's own buffers):
     the 4096^3 sparsity sweep of Section VI-B (TVW at 50 % is plain 2:4), uneven tiles from one
     magnitude threshold over all tile rows (Section V "load imbalance") launched longest first
     and in column order, TEW at 75 % with delta restored elements (Section VI, impact of delta),
     int8 TW / TVW against the dense int8 kernel and the fp16 launch of the same mask (Section
-    VI-B), and config 5's convolutions on the wide input against the materialised matrix."""
+    VI-B), a layer in 8 and in 4 bits (norm, quantiser, product, and the product by expert) against
+    its fp16 launch, and config 5's convolutions on the wide input against the materialised matrix."""
     def timed(fn, rounds=5):
         t_w = time.perf_counter()      # untimed: first touch of fresh buffers, clocks up after host-side packing
         while time.perf_counter() - t_w < PREWARM_S:
@@ -373,6 +375,63 @@ def extra_sweeps(tw, wl, torch, dev, stream, which, reps=24, sets=6):
                     p.free()
                 del A8, A16, C8, C16
         out["i8"] = rows
+    if "fewbit" in which:
+        rows = []
+        ptr = lambda bufs, r: bufs[r % len(bufs)].data_ptr()
+        for cfg, si in [(2, 0), (2, 1), (2, 2), (4, 0), (4, 1)]:
+            shp = wl.SHAPES[cfg][si]
+            M, K, N, G, sp = shp.M, shp.K, shp.N, 128, 0.75
+            nb = (K + 31) // 32
+            nsets = max(2, min(sets, int(600e6 // (M * (10 * K + 2 * N)))))
+            many = lambda shape, dtype: [torch.empty(shape, dtype=dtype, device=dev) for _ in range(nsets)]
+            B = wl.make_B(wl.seed_for(cfg, si), K, N, shp.sigma)
+            mask = wl.tw_mask(B, G, density=1.0 - sp, col_frac=0.10)
+            w_scale = np.abs(np.where(mask, B, 0).astype(np.float32)).max(axis=0) / 127 + 1e-12
+            B8 = np.rint(B / w_scale).clip(-127, 127).astype(np.int8)
+            # 4 bits: in each tile of G columns the quarter of the blocks of 32 rows with the largest sums of squares
+            mask4 = np.zeros((K, N), dtype=np.uint8)
+            for c in range(0, N, G):
+                score = [float((B[b * 32:b * 32 + 32, c:c + G].astype(np.float64) ** 2).sum()) for b in range(nb)]
+                for b in np.argsort(score)[int(nb * sp):]:
+                    mask4[b * 32:b * 32 + 32, c:c + G] = 1
+            p16 = [tw.tw_pack(B, mask, G, tw.PATTERN_TW) for _ in range(nsets)]
+            p8 = [tw.tw_pack_i8(B8, mask, G, tw.PATTERN_TW) for _ in range(nsets)]
+            p4 = [tw.tw_pack_mx4(B, mask4, G) for _ in range(nsets)]
+            X = [torch.randn((K, M), dtype=torch.float16, device=dev) for _ in range(nsets)]
+            R = [torch.randn((K, M), dtype=torch.float16, device=dev) for _ in range(nsets)]
+            H, C = many((K, M), torch.float16), many((N, M), torch.float16)
+            Q8, S8 = many((K, M), torch.int8), many((M,), torch.float32)
+            Q4, S4 = many((nb, M, 16), torch.uint8), many((nb, M), torch.uint8)
+            gamma = torch.ones(K, dtype=torch.float16, device=dev)
+            ws = torch.from_numpy(w_scale.astype(np.float32)).to(dev)
+
+            def norm_i8(r):
+                tw.tw_rmsnorm(ptr(X, r), ptr(R, r), gamma.data_ptr(), 1e-6, M, K, M, ptr(H, r), None, ptr(Q8, r), M, ptr(S8, r), stream)
+
+            def quant_mx4(r):
+                tw.tw_quant_mx4(ptr(X, r), M, K, M, tw.LAYOUT_KM, ptr(Q4, r), ptr(S4, r), M, stream)
+
+            t = dict(
+                fp16=timed(lambda r: tw.tw_gemm(ptr(X, r), M, M, tw.LAYOUT_KM, p16[r % nsets], ptr(C, r), M, stream)),
+                norm_i8=timed(norm_i8),
+                quant_i8=timed(lambda r: tw.tw_quant_i8(ptr(X, r), M, K, M, ptr(Q8, r), M, ptr(S8, r), stream)),
+                gemm_i8_scaled=timed(lambda r: tw.tw_gemm_i8_scaled(ptr(Q8, r), M, M, p8[r % nsets], ptr(S8, r), ws.data_ptr(),
+                                                                    ptr(C, r), M, stream)),
+                quant_mx4=timed(quant_mx4),
+                gemm_mx4=timed(lambda r: tw.tw_gemm_mx4(ptr(Q4, r), ptr(S4, r), M, M, p4[r % nsets], ptr(C, r), M, stream)))
+            # 8 experts of the same weight's kind: an eighth of the tokens each
+            experts = [tw.tw_concat([p4[i % nsets] for i in range(8)]) for _ in range(2)]
+            off = torch.tensor([M * e // 8 for e in range(9)], dtype=torch.int32, device=dev)
+            t["gemm_mx4_8_experts"] = timed(lambda r: tw.tw_gemm_mx4_grouped(ptr(Q4, r), ptr(S4, r), M, M, off.data_ptr(),
+                                                                             experts[r % 2], ptr(C, r), M, stream))
+            norm_bytes = M * K * 7 + 4 * M
+            rows.append(dict(shape=shp.name, M=M, K=K, N=N, G=G, sparsity=sp, **{k + "_us": round(v * 1e6, 2) for k, v in t.items()},
+                             norm_i8_GBps=round(norm_bytes / t["norm_i8"] / 1e9, 1),
+                             mx4_dense_eq_tflops=round(2.0 * M * K * N / t["gemm_mx4"] / 1e12, 1)))
+            for p in p16 + p8 + p4 + experts:
+                p.free()
+            del X, R, H, C, Q8, S8, Q4, S4
+        out["fewbit"] = rows
     return out
 
 
@@ -388,7 +447,7 @@ def main():
     ap.add_argument("--no-rows", action="store_true", help="skip the rows of the other configured workloads")
     ap.add_argument("--no-calibration", action="store_true")
     ap.add_argument("--extra", default="", help="comma list of opt-in sweeps, printed under `extra`: "
-                                                "cube, imbalance, tew, i8, conv, options (each takes 10-60 s)")
+                                                "cube, imbalance, tew, i8, fewbit, conv, options (each takes 10-60 s)")
     ap.add_argument("--calibrate", action="store_true", help="run the calibration kernels only and print their rates")
     ap.add_argument("--separate-qkv", action="store_true",
                     help="time the step with Q, K and V as three launches (6 launches per step)")
