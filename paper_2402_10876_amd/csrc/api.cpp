@@ -695,14 +695,26 @@ tw_status tw_dense_gemm(const void* A, const void* B, void* C, int M, int K, int
   return e == hipSuccess ? TW_OK : TW_ERR_HIP;
 }
 
-// int8 M-tile: 256 rows while that still gives every CU two workgroups, else 128.  The 64-row
-// instance (G = 128) is only used on request: it measured no better than 128 rows on the small
-// BERT-base launches and worse on the dense baseline.  As for fp16, 256 rows need kept-row lists of
-// at least 384 rows (1024 x 4096 at M = 8192 and 87.5 %, from HBM: 17.5 against 16.3 us).
-static int pick_tile_m_i8(const Opts& o, int M, int n_tiles, int G, int max_k) {
+// int8 M-tile: 256 rows while that still gives every CU two workgroups, else 128.  As for fp16, 256 rows
+// need kept-row lists of at least 384 rows (1024 x 4096 at M = 8192 and 87.5 %, from HBM: 17.5 against 16.3 us).
+// Condensed tiles of G = 128 (LDS holds three workgroups of 128 rows in a CU or two of 256; us of the scaled product / int8
+// output, from HBM):
+//   64 rows as long as every one has a CU to itself (64 / 128 rows: 768 x 768 at 75 %, M = 2048 4.6 / 5.5 and 4.0 / 4.7; 1024 x
+//   1024 at 50 %, M = 2048 5.9 / 6.9 and 5.0 / 6.0; 4096 x 4096 at 50 %, M = 512 15.0 / 15.5), and up to two for each with lists
+//   of up to 640 rows (768 x 768, M = 4096 5.4 / 5.7; 4096 x 4096 at 50 %, M = 1024 18.7 / 16.8);
+//   256 rows where they are one round and 128 rows are not (128 / 256 rows: 4096 x 4096 at 50 %, M = 4096 50.5 / 32.9 and
+//   47.5 / 31.8; 1024 x 4096 at 50 % 19.1 / 15.2 and 14.9 / 13.3; 768 x 2304 at 75 %, M = 6000 16.7 / 13.6 and 12.3 / 11.0; with
+//   one round of 128 rows 768 x 2304, M = 4096 8.0 / 9.6, with two of 256 M = 8192 14.0 / 18.1).
+// The dense baseline measured worse with 64 rows.
+static int pick_tile_m_i8(const Opts& o, int M, int n_tiles, int G, int max_k, bool dense) {
   const int forced = o.tile_m;
   if (forced == 128 || forced == 256 || (forced == 64 && G == 128)) return forced;
-  return (max_k >= 384 && (long)((M + 255) / 256) * n_tiles >= 512) ? 256 : 128;
+  const long wgs128 = (long)((M + 127) / 128) * n_tiles, wgs256 = (long)((M + 255) / 256) * n_tiles;
+  if (!dense && G == 128) {
+    if (wgs128 <= 128 || (wgs128 <= 256 && max_k <= 640)) return 64;
+    if (wgs128 > 768 && wgs256 <= 512) return 256;
+  }
+  return (max_k >= 384 && wgs256 >= 512) ? 256 : 128;
 }
 
 // The launch behind tw_gemm_i8 and tw_conv_gemm_i8 (conv: see gemm_launch).
@@ -736,7 +748,7 @@ static tw_status gemm_i8_launch(const void* A, int M, int lda, tw_handle_t h, vo
     e = twg::launch_tvw_i8(h->G, tm, g, (hipStream_t)stream);
   } else {
     // long K with too few tiles to fill the chip: split K inside the workgroup (as the fp16 path)
-    const int tm = pick_tile_m_i8(o, M, h->n_tiles > 0 ? h->n_tiles : 1, h->G, h->max_kp);
+    const int tm = pick_tile_m_i8(o, M, h->n_tiles > 0 ? h->n_tiles : 1, h->G, h->max_kp, false);
     const int ks = o.ksplit;
     int tmk = tm;
     e = hipErrorInvalidValue;
@@ -805,7 +817,7 @@ tw_status tw_dense_gemm_i8(const void* A, const void* B, void* C, int M, int K, 
   g.n_tiles = (N + tn - 1) / tn;
   const Opts o = default_opts();
   g.xcd_map = o.xcd_map ? 1 : 0;
-  hipError_t e = twg::launch_dense_i8(tn, pick_tile_m_i8(o, M, g.n_tiles, tn, K), g, (hipStream_t)stream);
+  hipError_t e = twg::launch_dense_i8(tn, pick_tile_m_i8(o, M, g.n_tiles, tn, K, true), g, (hipStream_t)stream);
   if (e == hipErrorInvalidValue) return TW_ERR_UNSUPPORTED;
   return e == hipSuccess ? TW_OK : TW_ERR_HIP;
 }

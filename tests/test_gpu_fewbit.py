@@ -258,6 +258,38 @@ def test_gemm_i8_scaled(M, K, N, G, pattern):
     assert not np.signbit(got[~mask.any(0), :M]).any()
 
 
+@pytest.mark.parametrize("M,N", [(50, 300), (900, 1500), (2000, 1500), (4100, 2500), (4090, 3900)])
+@pytest.mark.parametrize("tile_m", [0, 64, 128, 256])
+def test_int8_tiles_of_every_height(tile_m, M, N):
+    """The same whole sums with every height of the tiles, chosen or asked for, in the three types of output."""
+    import torch
+    rng = np.random.default_rng(M)
+    K, G = 200, 128
+    mask = random_tw_mask(rng, K, N, G)
+    A, B = wl.rng_i8(M, (M, K)), wl.rng_i8(K, (K, N))
+    ld = up(M, 16)
+    Ad = torch.zeros((K, ld), dtype=torch.int8, device="cuda")
+    Ad[:, :M] = torch.from_numpy(np.ascontiguousarray(A.T)).cuda()
+    sa, sw = (rng.random(M) * 0.01).astype(np.float32), (rng.random(N) * 0.01).astype(np.float32)
+    sad, swd = torch.from_numpy(sa).cuda(), torch.from_numpy(sw).cuda()
+    out = [torch.empty((N, ld), dtype=t, device="cuda") for t in (torch.int32, torch.int8, torch.float16)]
+    p = tw.tw_pack_i8(B, mask, G, tw.PATTERN_TW)
+    print(f"int8 tiles tile_m={tile_m} M={M} N={N}", flush=True)
+    tw.tw_set_option("tile_m", tile_m)
+    try:
+        for dtype in (0, 1):
+            tw.tw_gemm_i8(Ad.data_ptr(), M, ld, p, out[dtype].data_ptr(), ld, dtype, 1e-3, _stream())
+        tw.tw_gemm_i8_scaled(Ad.data_ptr(), M, ld, p, sad.data_ptr(), swd.data_ptr(), out[2].data_ptr(), ld, _stream())
+    finally:
+        tw.tw_set_option("tile_m", 0)
+    got = [o.cpu().numpy()[:, :M].T for o in out]
+    p.free()
+    sums = np.rint(A.astype(np.float64) @ (B * (mask != 0)).astype(np.float64))
+    assert np.array_equal(got[0], sums.astype(np.int32))
+    assert np.array_equal(got[1], np.clip(np.rint(sums.astype(np.float32) * np.float32(1e-3)), -128, 127).astype(np.int8))
+    assert np.array_equal(got[2], ofb.gemm_i8_scaled(sums, sa, sw))
+
+
 # ---- microscaled 4-bit -----------------------------------------------------------------------------
 def _same_codes(Q, S, X, ldq):
     M, K = X.shape
