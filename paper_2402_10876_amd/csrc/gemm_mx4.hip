@@ -167,15 +167,36 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB == 8 ? 2 : 1)) void gem
     }
   };
   auto load = [&](int s, Step& x) { load_a(s, x); load_w(s, x); };
+  auto multiply_row = [&](int i, const Step& x, int sb) {
+    acc[i][0] = mfma4<0>(x.a[i], x.b[0], acc[i][0], x.sa[i], sb);
+    if constexpr (NB > 1) acc[i][1] = mfma4<1>(x.a[i], x.b[1], acc[i][1], x.sa[i], sb);
+    if constexpr (NB > 2) acc[i][2] = mfma4<2>(x.a[i], x.b[2], acc[i][2], x.sa[i], sb);
+    if constexpr (NB > 3) acc[i][3] = mfma4<3>(x.a[i], x.b[3], acc[i][3], x.sa[i], sb);
+  };
   auto multiply = [&](const Step& x) {
     const int sb = (int)((uint32_t)x.sb >> (8 * nb0));
 #pragma unroll
+    for (int i = 0; i < MB; ++i) multiply_row(i, x, sb);
+  };
+
+  // multiply and load in one, the loads in between the products: the order that a wave holds which is alone on its SIMD.  Left to
+  // itself the compiler gathers the loads of all D steps behind their products and waits for all at once (4096 x 4096, M =
+  // 8192, 82.3 against 78.3 us, half 49.3 against 46.4; shapes with more waves on a SIMD lose 1 to 5 % by it).
+  constexpr bool HOLD = MB * NB == 16;
+  auto multiply_load = [&](Step& x, int s) {
+    const int sb = (int)((uint32_t)x.sb >> (8 * nb0));
+    const uint32_t b = list[2 * s + half];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
     for (int i = 0; i < MB; ++i) {
-      acc[i][0] = mfma4<0>(x.a[i], x.b[0], acc[i][0], x.sa[i], sb);
-      if constexpr (NB > 1) acc[i][1] = mfma4<1>(x.a[i], x.b[1], acc[i][1], x.sa[i], sb);
-      if constexpr (NB > 2) acc[i][2] = mfma4<2>(x.a[i], x.b[2], acc[i][2], x.sa[i], sb);
-      if constexpr (NB > 3) acc[i][3] = mfma4<3>(x.a[i], x.b[3], acc[i][3], x.sa[i], sb);
+      multiply_row(i, x, sb);
+      __builtin_amdgcn_sched_barrier(0);
+      x.a[i] = *(const int4v*)(g.Q + (uint64_t)b * ldq * 16u + tok[i] * 16u);
+      x.sa[i] = g.S[(uint64_t)b * ldq + tok[i]];
+      __builtin_amdgcn_sched_barrier(0);
     }
+    load_w(s, x);
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   // D steps under way: the wave's steps are wk, wk + WK, .. (n of them)
@@ -193,8 +214,12 @@ __global__ __launch_bounds__(64 * WM * WN * WK, (MB * NB == 8 ? 2 : 1)) void gem
     for (; i + 2 * D <= n; i += D)
 #pragma unroll
       for (int d = 0; d < D; ++d) {
-        multiply(st[d]);
-        load(wk + (i + D + d) * WK, st[d]);
+        if constexpr (HOLD) {
+          multiply_load(st[d], wk + (i + D + d) * WK);
+        } else {
+          multiply(st[d]);
+          load(wk + (i + D + d) * WK, st[d]);
+        }
       }
 #pragma unroll
     for (int d = 0; d < D; ++d)
@@ -294,14 +319,15 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 #ifndef TUNE
 // Tile shapes, tokens x columns (waves, how the work is shared), us per launch in a captured stream of launches, operands from
 // HBM, K x N and the share of the blocks kept:
-//   R 256 x 128 (2)       wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
+//   R 512 x 128 (4)       wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
 //   Q 256 x 128 (4)       wave tiles of 64 x 128: more waves to hide the ends of short lists
 //   P 128 x 128 (4)
 //   W  64 x 128 (2)
 //   U  32 x 128 (2)
 //   S  32 x 32 (4 on shares of the list), S2 64 x 32 (2 x 4)
-// Large: 4096 x 4096, all, M = 8192 R 78.6, Q 84.4, P 110; half, R 50.4, Q 48.3; 1024 x 4096, half, M = 4096 Q 12.9, P 13.5, R 15+.
-// From 384 tiles of 256 rows on: fewer leave CUs idle (2048 x 1024, half, M = 8192, 256 tiles: P 10.4, Q 10.8; 1024 x 1024
+// Large: 4096 x 4096, all, M = 8192 R 77.2, Q 94.7, P 122 (R of two waves 80.9); half, R 46.2, Q 55.3; M = 4096 R 24.1, Q 26.5, M =
+// 3100 23.7, 23.3; 1024 x 4096, all (16 steps), M = 8192 R 34.4, Q 35.5, M = 4096 16.8, 16.4; half (8 steps) 26.6, 24.6 and 14.8,
+// 13.4; 8192 cubed R 263.  From 384 tiles of 256 rows on: fewer leave CUs idle (2048 x 1024, half, M = 8192, 256 tiles: P 10.4, Q 10.8; 1024 x 1024
 // P 7.6, Q 8.9).  From 200 tiles of P on: 2048 x 2048, half, M = 2048 P 7.5, U 7.5; 4096 x 4096, half, M = 1024 P 10.7,
 // U 11.9; 1024 x 4096, half, M = 512 (128 tiles) P 5.6, U 5.4; 1024 x 1024, M = 1024 P 4.7, U 3.7.
 // Lists shared among waves where tiles of 64 rows would be fewer than 160 and a list is long: 4096 x 4096, half, M = 128
@@ -320,13 +346,13 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
   } else {
     auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
     if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles(32) * 4 <= 256 ? S : S2;
-    else if (tiles(256) >= 384) shape = steps >= 32 ? R : Q;
+    else if (tiles(256) >= 384) shape = steps >= (tiles(256) > 512 ? 16 : 32) ? R : Q;
     else shape = tiles(128) >= 200 ? P : U;
   }
   if (shape == S) return launch_mx4<GB, 1, 1, 1, 1, 4, 4>(g, stream);
   if (shape == S2) return launch_mx4<GB, 1, 1, 2, 1, 4, 4>(g, stream);
   if constexpr (GB == 4) {
-    if (shape == R) return launch_mx4<4, 4, 4, 2, 1, 1, 3>(g, stream);
+    if (shape == R) return launch_mx4<4, 4, 4, 4, 1, 1, 3>(g, stream);
     if (shape == Q) return launch_mx4<4, 2, 4, 4, 1, 1, 2>(g, stream);
     if (shape == P) return launch_mx4<4, 2, 2, 2, 2, 1, 4>(g, stream);
     if (shape == W) return launch_mx4<4, 2, 2, 1, 2, 1, 3>(g, stream);

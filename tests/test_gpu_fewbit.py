@@ -369,6 +369,24 @@ def test_gemm_mx4(M, K, N, G, mask):
     assert not dropped.any() and not np.signbit(dropped).any()
 
 
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (3001, 700, 1290), (600, 2000, 900)])
+def test_gemm_mx4_of_many_tokens(M, K, N, G):
+    """The tile shapes of larger products: 512 and 256 rows, with long and short lists, 128 rows, lists shared among waves."""
+    rng = np.random.default_rng(M + K)
+    m = block_mask(rng, K, N, G, 1.0, 0.95)
+    B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
+    X = acts(M, M, K)
+    X[M - 2, K // 3] = np.inf
+    Q, S = fu.quant_mx4_dev(tw, X, tw.LAYOUT_MK, _stream())
+    p = tw.tw_pack_mx4(B, m, G)
+    print(f"gemm_mx4 M={M} K={K} N={N} G={G}", flush=True)
+    C = _gemm_mx4(p, Q, S, M, N)
+    p.free()
+    codes, scale = ofb.mx4_quant(np.ascontiguousarray(X.T))
+    fu.assert_mx4_close(C, codes, scale, B, m, G)
+
+
 def test_gemm_mx4_identity_returns_the_weight():
     """One-hot tokens: C is the packed weight exactly, so every lane, block and scale is in its place."""
     rng = np.random.default_rng(8)
@@ -418,6 +436,9 @@ def _grouped(h, Q, S, M, N, off, ldc=None):
     (1003, 515, 128, [0, 0, 0, 700]),
     (64, 64, 64, [2, 9]),
     (160, 300, 64, [0, 1000, 1001, 1013, 2100]),
+    (200, 600, 128, [0, 1500, 1511, 4000, 4063, 5000, 6200, 7000, 7995]),
+    (1030, 2100, 128, [5, 4000, 8190]),
+    (500, 1500, 64, [5, 4100, 8190]),
     (128, 128, 128, [0] + sorted(np.random.default_rng(1).integers(0, 400, 79).tolist()) + [400]),
 ])
 def test_grouped(K, N, G, off):
