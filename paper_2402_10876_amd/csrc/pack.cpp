@@ -221,71 +221,94 @@ tw_status pack_host(const uint16_t* B, const uint8_t* mask, const uint8_t* tile_
 }
 
 static void build_mx4_lists(tw_handle_s* h);
-static void build_mx4_values(tw_handle_s* h);
 
 // Microscaled 4-bit weights: kept columns are those with any mask bit, cut into tiles of G; a tile keeps a block of 32 rows
 // whole if the mask keeps anything of it there.  `values` are what the blocks stand for (fp16).
 tw_status pack_mx4_host(const uint16_t* B, const uint8_t* mask, int K, int N, int G, tw_handle_s* h) try {
   h->K = K; h->N = N; h->G = G; h->pattern = TW_PATTERN_TW; h->dtype = TW_DTYPE_MX4;
-  std::vector<int32_t> rows, offs;
-  structure_of(mask, K, N, G, h->col_idx, offs, rows);
-  const int n_tiles = (int)offs.size() - 1, KB = (K + MX4_BLOCK - 1) / MX4_BLOCK;
+  const int KB = (K + MX4_BLOCK - 1) / MX4_BLOCK;
+  std::vector<uint8_t> any((size_t)KB * N, 0), col_any(N, 0);        // per block of rows and per column
+  for (int b = 0; b < KB; ++b) {
+    uint8_t* to = any.data() + (size_t)b * N;
+    for (int k = b * MX4_BLOCK; k < std::min(K, (b + 1) * MX4_BLOCK); ++k) {
+      const uint8_t* r = mask + (size_t)k * N;
+      for (int n = 0; n < N; ++n) to[n] |= r[n];
+    }
+    for (int n = 0; n < N; ++n) col_any[n] |= to[n];
+  }
+  for (int n = 0; n < N; ++n)
+    if (col_any[n]) h->col_idx.push_back(n);
+  const int n_kept = (int)h->col_idx.size(), n_tiles = (n_kept + G - 1) / G;
   h->tile_k_off.assign(1, 0);
-  std::vector<uint8_t> kept(KB);
-  for (int t = 0; t < n_tiles; ++t) {          // whole blocks
-    std::fill(kept.begin(), kept.end(), 0);
-    for (int i = offs[t]; i < offs[t + 1]; ++i) kept[rows[i] / MX4_BLOCK] = 1;
-    for (int b = 0; b < KB; ++b)
-      if (kept[b])
-        for (int k = b * MX4_BLOCK; k < std::min(K, (b + 1) * MX4_BLOCK); ++k) h->row_idx.push_back(k);
+  for (int t = 0; t < n_tiles; ++t) {
+    const int32_t *c0 = h->col_idx.data() + (size_t)t * G, *c1 = h->col_idx.data() + std::min(n_kept, (t + 1) * G);
+    for (int b = 0; b < KB; ++b) {
+      const uint8_t* r = any.data() + (size_t)b * N;
+      if (std::none_of(c0, c1, [r](int32_t c) { return r[c] != 0; })) continue;
+      for (int k = b * MX4_BLOCK; k < std::min(K, (b + 1) * MX4_BLOCK); ++k) h->row_idx.push_back(k);
+    }
     h->tile_k_off.push_back((int32_t)h->row_idx.size());
   }
   set_tiles_of_G(h);
   finish_lists(h);
+  build_mx4_lists(h);
   uint16_t value[256][16];                     // fp16 bits of a code under a scale byte (those of finite blocks)
   for (int s = MX4_ONE - 26; s <= MX4_ONE + 13; ++s)
     for (int c = 0; c < 16; ++c) value[s][c] = mx4_value((uint8_t)c, (uint8_t)s);
   h->values.resize((size_t)h->sum_kw);
-  uint16_t top[128];
-  uint8_t scale[128];
+  Mx4Image& d = h->mx4;
+  const int GB = G / 32;
+  int64_t s0 = 0;                              // first step of the tile
+  for (const Mx4Tile& r : d.tiles) s0 += r.steps;
+  d.vals.assign((size_t)s0 * GB * 1024, 0);
+  d.scales.assign((size_t)s0 * GB * 64, (uint8_t)MX4_ONE);
+  uint16_t x[MX4_BLOCK][128], top[128];
+  uint8_t code[MX4_BLOCK][128], scale[128];
   float factor[128];
   for (int t = 0; t < n_tiles; ++t) {
     const int w = h->tile_col_off[t + 1] - h->tile_col_off[t];
     const int32_t* cols = h->col_idx.data() + h->tile_col_off[t];
+    const bool run = cols[w - 1] - cols[0] == w - 1;           // neighbours: read in a row
     uint16_t* v = h->values.data() + h->val_off[t];
-    for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1];) {
+    s0 = d.tiles[t].step0;
+    int b = 0;
+    for (int i = h->tile_k_off[t]; i < h->tile_k_off[t + 1]; ++b) {
       const int k0 = h->row_idx[i], n = std::min(K - k0, MX4_BLOCK);
       std::fill(top, top + w, (uint16_t)0);
       for (int k = 0; k < n; ++k) {
-        const size_t row = (size_t)(k0 + k) * N;
-        for (int c = 0; c < w; ++c) {
-          const uint16_t x = mask[row + cols[c]] ? B[row + cols[c]] : (uint16_t)0;
-          v[(size_t)k * w + c] = x;
-          top[c] = std::max(top[c], (uint16_t)(x & 0x7fff));
-        }
+        const uint16_t* from = B + (size_t)(k0 + k) * N;
+        const uint8_t* keep = mask + (size_t)(k0 + k) * N;
+        if (run)
+          for (int c = 0; c < w; ++c) x[k][c] = keep[cols[0] + c] ? from[cols[0] + c] : (uint16_t)0;
+        else
+          for (int c = 0; c < w; ++c) x[k][c] = keep[cols[c]] ? from[cols[c]] : (uint16_t)0;
+        for (int c = 0; c < w; ++c) top[c] = std::max(top[c], (uint16_t)(x[k][c] & 0x7fff));
       }
+      for (int k = n; k < MX4_BLOCK; ++k) std::fill(x[k], x[k] + w, (uint16_t)0);
+      const int64_t s = s0 + b / 2;
       for (int c = 0; c < w; ++c) {
         if (top[c] >= 0x7c00) return TW_ERR_ARG;
         scale[c] = mx4_scale_of(top[c]);
         factor[c] = mx4_factor(scale[c]);
+        d.scales[((size_t)s * 64 + c % 32 + 32 * (b % 2)) * GB + c / 32] = scale[c];
       }
-      for (int k = 0; k < n; ++k)
-        for (int c = 0; c < w; ++c) {
-          uint16_t& x = v[(size_t)k * w + c];
-          x = value[scale[c]][mx4_code(x, factor[c])];
-        }
-      v += (size_t)n * w;
+      for (int k = 0; k < MX4_BLOCK; ++k)
+        for (int c = 0; c < w; ++c) code[k][c] = mx4_code(x[k][c], factor[c]);
+      for (int k = 0; k < n; ++k, v += w)
+        for (int c = 0; c < w; ++c) v[c] = value[scale[c]][code[k][c]];
+      for (int c = 0; c < w; ++c) {
+        uint8_t* out = d.vals.data() + (((size_t)s * GB + c / 32) * 64 + c % 32 + 32 * (b % 2)) * 16;
+        for (int k = 0; k < 16; ++k) out[k] = (uint8_t)(code[2 * k][c] | code[2 * k + 1][c] << 4);
+      }
       i += n;
     }
   }
-  build_mx4_lists(h);
-  build_mx4_values(h);
   return TW_OK;
 } catch (const std::bad_alloc&) {
   return TW_ERR_ALLOC;
 }
 
-// The image of a microscaled 4-bit weight from its logical form (layout at Mx4Image): the lists, then the values.
+// The lists of a microscaled 4-bit weight's image from its logical form (layout at Mx4Image).
 static void build_mx4_lists(tw_handle_s* h) {
   Mx4Image& d = h->mx4;
   const int G = h->G;
@@ -339,45 +362,6 @@ static void build_mx4_lists(tw_handle_s* h) {
       step += r.steps;
       for (int c = h->tile_col_off[t]; c < h->tile_col_off[t + 1]; ++c) d.col_idx[at * G + c - h->tile_col_off[t]] = h->col_idx[c];
     }
-  }
-}
-
-static void build_mx4_values(tw_handle_s* h) {
-  Mx4Image& d = h->mx4;
-  const int GB = h->G / 32;
-  int64_t steps = 0, s0 = 0;
-  for (const Mx4Tile& r : d.tiles) steps += r.steps;
-  d.vals.assign((size_t)steps * GB * 1024, 0);
-  d.scales.assign((size_t)steps * GB * 64, (uint8_t)MX4_ONE);
-  uint16_t top[128];
-  float factor[128];
-  uint8_t code[MX4_BLOCK][128];
-  for (int tl = 0; tl < h->n_tiles; ++tl) {    // (the tiles that fill up have no steps)
-    const int w = h->tile_col_off[tl + 1] - h->tile_col_off[tl];
-    const uint16_t* v = h->values.data() + h->val_off[tl];
-    int b = 0;
-    for (int i = h->tile_k_off[tl]; i < h->tile_k_off[tl + 1]; ++b) {
-      const int n = std::min(h->K - h->row_idx[i], MX4_BLOCK);
-      const int64_t s = s0 + b / 2;
-      std::fill(top, top + w, (uint16_t)0);
-      for (int k = 0; k < n; ++k)
-        for (int c = 0; c < w; ++c) top[c] = std::max(top[c], (uint16_t)(v[(size_t)k * w + c] & 0x7fff));
-      for (int c = 0; c < w; ++c) {
-        const uint8_t sc = mx4_scale_of(top[c]);
-        d.scales[((size_t)s * 64 + c % 32 + 32 * (b % 2)) * GB + c / 32] = sc;
-        factor[c] = mx4_factor(sc);
-      }
-      for (int k = 0; k < n; ++k)
-        for (int c = 0; c < w; ++c) code[k][c] = mx4_code(v[(size_t)k * w + c], factor[c]);
-      for (int k = n; k < MX4_BLOCK; ++k) std::fill(code[k], code[k] + w, (uint8_t)0);
-      for (int c = 0; c < w; ++c) {
-        uint8_t* out = d.vals.data() + (((size_t)s * GB + c / 32) * 64 + c % 32 + 32 * (b % 2)) * 16;
-        for (int k = 0; k < 16; ++k) out[k] = (uint8_t)(code[2 * k][c] | code[2 * k + 1][c] << 4);
-      }
-      v += (size_t)n * w;
-      i += n;
-    }
-    s0 += (b + 1) / 2;
   }
 }
 
