@@ -19,6 +19,38 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #define LDS_PTR(T, p) ((T __attribute__((address_space(3)))*)(p))
 #define GLOBAL_PTR(p) ((const __attribute__((address_space(1))) void*)(p))
 
+// The first n (1 .. 7) of eight fp16 values at a 16-byte aligned address, in stores of 4, 2 and 1.
+__device__ __forceinline__ void store_front(_Float16* p, half8 v, int n) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  uint32_t a = w[0], b = w[1];
+  if (n & 4) {
+    *(uint2*)p = make_uint2(a, b);
+    a = w[2];
+    b = w[3];
+  }
+  if (n & 2) {
+    *(uint32_t*)(p + (n & 4)) = a;
+    a = b;
+  }
+  if (n & 1) *(uint16_t*)(p + (n & 6)) = (uint16_t)a;
+}
+// The last n (1 .. 7) of them.
+__device__ __forceinline__ void store_back(_Float16* p, half8 v, int n) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  uint32_t a = w[2], b = w[3];
+  if (n & 4) {
+    *(uint2*)(p + 4) = make_uint2(a, b);
+    a = w[0];
+    b = w[1];
+  }
+  const int at = n & 4 ? 4 : 8;          // values from here on are in memory
+  if (n & 2) {
+    *(uint32_t*)(p + at - 2) = b;
+    b = a;
+  }
+  if (n & 1) *(uint16_t*)(p + at - (n & 2) - 1) = (uint16_t)(b >> 16);
+}
+
 constexpr int KS = 32;        // condensed rows per main-loop stage
 constexpr int NTHREADS = 256;
 

@@ -454,11 +454,7 @@ __global__ __launch_bounds__(NWAVES * 64, (TM * TN >= 256 * 128) ? 2 : 1) void t
       if (cols[i] < 0 || m >= g.M) continue;
       _Float16* dst = (_Float16*)g.C + (size_t)cols[i] * g.ldc + m;
       if (m + 8 <= g.M) __builtin_nontemporal_store(pc[i], (half8*)dst);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (m + e < g.M) dst[e] = pc[i][e];
-      }
+      else store_front(dst, pc[i], g.M & 7);
     }
   } else if constexpr (OUT == OUT_I8) {
     // ---- epilogue, int8 output: requantise in registers, stage the whole tile as bytes

@@ -355,12 +355,12 @@ __global__ __launch_bounds__(256) void tvw_gemm_i8_kernel(GemmI8Args g) {
     if (cols[i] < 0 || m >= g.M) continue;
     char* dst = (char*)g.C + ((size_t)cols[i] * g.ldc + m) * ES;
     if (m + CH <= g.M) __builtin_nontemporal_store(pc[i], (int4v*)dst);
+    else if constexpr (OUT == OUT_F16) store_front((_Float16*)dst, __builtin_bit_cast(half8, pc[i]), g.M & 7);
     else {
 #pragma unroll
       for (int e = 0; e < CH; ++e)
         if (m + e < g.M) {
-          if constexpr (OUT == OUT_F16) ((uint16_t*)dst)[e] = (uint16_t)(pc[i][e >> 1] >> (16 * (e & 1)));
-          else if constexpr (OUT == OUT_I8) dst[e] = (char)(pc[i][e >> 2] >> (8 * (e & 3)));
+          if constexpr (OUT == OUT_I8) dst[e] = (char)(pc[i][e >> 2] >> (8 * (e & 3)));
           else ((int*)dst)[e] = pc[i][e];
         }
     }

@@ -69,20 +69,27 @@ __device__ __forceinline__ uint2 round8(const float (&f)[8], const float (&mul)[
   }
   return make_uint2(q[0], q[1]);
 }
-// Eight tokens of a row to memory; only the first `tail` of the piece that ends behind the last token.
+// Eight tokens of a row to memory; only the first `tail` of the piece that ends behind the last token, in stores of 4, 2 and 1
+// (one by one they made the workgroup of that piece the last: int8 quantiser, 1003 rows, 1957 tokens 7.2 us, 1968 tokens 5.6).
 __device__ __forceinline__ void store8(_Float16* p, half8 v, bool whole, int tail) {
   if (whole) *(half8*)p = v;
-  else
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < tail) p[e] = v[e];
+  else store_front(p, v, tail);
 }
 __device__ __forceinline__ void store8(int8_t* p, uint2 q, bool whole, int tail) {
-  if (whole) *(uint2*)p = q;
-  else
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < tail) p[e] = (int8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+  if (whole) {
+    *(uint2*)p = q;
+    return;
+  }
+  uint32_t a = q.x;
+  if (tail & 4) {
+    *(uint32_t*)p = a;
+    a = q.y;
+  }
+  if (tail & 2) {
+    *(uint16_t*)(p + (tail & 4)) = (uint16_t)a;
+    a >>= 16;
+  }
+  if (tail & 1) p[tail & 6] = (int8_t)a;
 }
 
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {

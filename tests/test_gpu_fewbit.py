@@ -72,6 +72,16 @@ def test_norm(M, K):
     _check_norm(X, R, None, 1e-6, i8=False, f16=True, H=False)
 
 
+@pytest.mark.parametrize("M", list(range(2, 17)) + list(range(1530, 1537)))
+def test_norm_of_any_number_of_tokens(M):
+    """The last piece of 8 tokens holds 1 to 8 of them; with many long tokens the slices of the rows do."""
+    K = 41 if M < 100 else 2100
+    print(f"norm M={M} K={K}", flush=True)
+    X, R = acts(M + K, M, K), acts(M + K + 1, M, K, 3.0)
+    _check_norm(X, R, None, 1e-5, i8=True, f16=True)
+    _check_norm(X, R, None, 1e-5, i8=False, f16=True)
+
+
 @pytest.mark.parametrize("M,K", [(2049, 64), (2500, 1100), (2200, 2100), (4097, 40), (4100, 1030), (4098, 2050), (8200, 300),
                                  (16321, 2049), (16500, 2049), (16450, 96)])
 def test_norm_and_quantiser_of_many_tokens(M, K):
@@ -290,6 +300,16 @@ def test_int8_tiles_of_every_height(tile_m, M, N):
     assert np.array_equal(got[2], ofb.gemm_i8_scaled(sums, sa, sw))
 
 
+@pytest.mark.parametrize("pattern", ["tw", "tvw"])
+@pytest.mark.parametrize("M", list(range(193, 201)))
+def test_gemm_i8_scaled_of_any_number_of_tokens(M, pattern):
+    tw.tw_set_option("tile_m", 64)           # (not the kernel for few tokens)
+    try:
+        test_gemm_i8_scaled(M, 140, 150, 128, pattern)
+    finally:
+        tw.tw_set_option("tile_m", 0)
+
+
 # ---- microscaled 4-bit -----------------------------------------------------------------------------
 def _same_codes(Q, S, X, ldq):
     M, K = X.shape
@@ -387,6 +407,20 @@ def test_gemm_mx4_of_many_tokens(M, K, N, G):
     fu.assert_mx4_close(C, codes, scale, B, m, G)
 
 
+def test_gemm_mx4_of_any_number_of_tokens():
+    rng = np.random.default_rng(12)
+    K, N, G = 70, 90, 64
+    m = block_mask(rng, K, N, G)
+    B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
+    p = tw.tw_pack_mx4(B, m, G)
+    for M in range(1, 18):
+        X = acts(M, M, K)
+        Q, S = fu.quant_mx4_dev(tw, X, tw.LAYOUT_KM, _stream())
+        codes, scale = ofb.mx4_quant(np.ascontiguousarray(X.T))
+        fu.assert_mx4_close(_gemm_mx4(p, Q, S, M, N), codes, scale, B, m, G)
+    p.free()
+
+
 def test_gemm_mx4_identity_returns_the_weight():
     """One-hot tokens: C is the packed weight exactly, so every lane, block and scale is in its place."""
     rng = np.random.default_rng(8)
@@ -436,6 +470,8 @@ def _grouped(h, Q, S, M, N, off, ldc=None):
     (1003, 515, 128, [0, 0, 0, 700]),
     (64, 64, 64, [2, 9]),
     (160, 300, 64, [0, 1000, 1001, 1013, 2100]),
+    (96, 130, 128, np.cumsum([0] + list(range(1, 18)) + list(range(70, 78))).tolist()),
+    (96, 130, 64, [3] + [12 + 8 * i for i in range(9)] + [141]),
     (200, 600, 128, [0, 1500, 1511, 4000, 4063, 5000, 6200, 7000, 7995]),
     (1030, 2100, 128, [5, 4000, 8190]),
     (500, 1500, 64, [5, 4100, 8190]),
