@@ -10,6 +10,8 @@ What it holds, each piece written out plainly in NumPy fp64 / Python ints:
             (Section III-A problem statement; Section V "skips computing
             partial sums for pruned elements"), plus a brute-force per-element
             version that pins it.
+  fewbit.py the operators around products in 8 and 4 bits: root-mean-square norm, quantisers,
+            scaled int8 products, microscaled 4-bit products, plain and by expert.
   prune.py  one-shot TW / VW(2:4) / TVW mask construction following the steps
             of Algorithms 2 and 3 with magnitude scores.
   pack.py   the canonical *logical* packed form: kept-column list, per-tile
