@@ -322,51 +322,67 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 }
 
 #ifndef TUNE
-// Tile shapes, tokens x columns (waves, how the work is shared), us per launch in a captured stream of launches, operands from
-// HBM, K x N and the share of the blocks kept:
-//   R 512 x 128 (4)       wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
-//   Q 256 x 128 (4)       wave tiles of 64 x 128: more waves to hide the ends of short lists
-//   P 128 x 128 (4)
-//   W  64 x 128 (2)
-//   U  32 x 128 (2)
-//   S  32 x 32 (4 on shares of the list), S2 64 x 32 (2 x 4)
-// Large: 4096 x 4096, all, M = 8192 R 77.2, Q 94.7, P 122 (R of two waves 80.9); half, R 46.2, Q 55.3; M = 4096 R 24.1, Q 26.5, M =
-// 3100 23.7, 23.3; 1024 x 4096, all (16 steps), M = 8192 R 34.4, Q 35.5, M = 4096 16.8, 16.4; half (8 steps) 26.6, 24.6 and 14.8,
-// 13.4; 8192 cubed R 263.  From 384 tiles of 256 rows on: fewer leave CUs idle (2048 x 1024, half, M = 8192, 256 tiles: P 10.4, Q 10.8; 1024 x 1024
-// P 7.6, Q 8.9).  From 200 tiles of P on: 2048 x 2048, half, M = 2048 P 7.5, U 7.5; 4096 x 4096, half, M = 1024 P 10.7,
-// U 11.9; 1024 x 4096, half, M = 512 (128 tiles) P 5.6, U 5.4; 1024 x 1024, M = 1024 P 4.7, U 3.7.
+// Tile shapes, tokens x columns (waves), us per launch in a captured stream of launches, operands from HBM, K x N and
+// the share of the blocks kept:
+//   R 512 x 128 (4)   wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
+//   Q 256 x 128 (4)   wave tiles of 64 x 128
+//   V  64 x 128 (1)   W  64 x 64 (1)   U  32 x 64 (1)   waves on their own: none waits for another
+//   P 128 x 128 (4)   wave tiles of 64 x 64
+//   S  32 x 32 (4 on shares of the list)   S2 64 x 32 (2 x 4)
+// R for long lists: 4096 x 4096, all, M = 8192 R 77, Q 95; half, R 46, Q 55; M = 4096 R 25.7, Q 28.6, V 28.4; M = 3100 24.8, 25.0, 24.3;
+// 1024 x 4096, all (16 steps), M = 8192 R 34.4, Q 35.5, M = 4096 16.8, 16.4; half (8 steps) 26.6, 24.6 and 14.8, 13.4; 8192 cubed
+// R 263.  Else up to about a round and a half of 256 rows V, above Q: 1024 x 4096, half, M = 3100 V 12.3, Q 12.7, M = 6000 22.9,
+// 23.6, M = 8192 27.2, 25.5; 2048 x 2048, half, M = 6000 V 14.3, Q 16.2, P 15.2.  Of the small ones by how many there are (a
+// CU takes four to five waves of W in the time of two or three larger tiles): 4096 x 4096, half, M = 2500 V 21.3, W 22.6, M = 2048 V
+// 16.7, W 16.7, U 22.8, M = 1536 V 15.9, W 14.3, U 17.7; 1024 x 1024, half, M = 10000 V 10.1, W 10.0, U 10.8, M = 5000 W 7.5, U
+// 7.4, M = 3300 W 6.7, U 5.9, P 6.4.  One round of P, long lists: 4096 x 4096, half, M = 1024 P 11.3, W 12.6, U 13.1, 4096 x 2048, M =
+// 1700 10.5, 12.4, 10.8; short ones 1024 x 4096, M = 1024 6.9, 7.2, 6.8.
 // Lists shared among waves where tiles of 64 rows would be fewer than 160 and a list is long: 4096 x 4096, half, M = 128
 // S2 5.2, S 6.0, U 7.6; all, M = 256 S2 10.5, U 12.0; 4096 x 1024, all, M = 512 S2 6.9, U 10; up to 256 tiles of S it has
 // the shortest way: 1024 x 1024, half, M = 256 S 3.0, S2 3.1, U 3.4; 4096 x 4096, M = 1 S 3.7, S2 4.3.
-// By expert, where ranges end inside tiles: 2048 x 1024, half, 8 experts, M = 8192 W 13.7, U 15.4, P 16.1; M = 2048 U 8.0,
-// W 9.0; M = 512 S 6.2, U 7+; 1024 x 1024, 32 experts, M = 4000 W 10.0, U 10.6; M = 1000 U 7.8, S 9.7.
+// By expert, where ranges end inside tiles (half kept): 2048 x 1024, 8 experts, M = 8192 W 13.1, V 14.4, U 15.2, Q 16.7, M = 6000 W
+// 11.2, U 12.1, M = 2048 U 7.2, W 8.3, M = 512 S 5.7, U 6.2; 1024 x 1024, 8 experts, M = 12000 V 12.7, W 13.7; 1024 x 4096, 8 experts,
+// M = 8192 V 33, W 37, Q 34; 4096 x 2048, 16 experts, M = 5000 V 32, W 39.  Few tokens each: 1024 x 1024, 32 experts, M = 4000 U 9.0, W
+// 9.7, M = 8000 U 12.4, W 12.2; 256 experts, M = 16384 V 48, U 50, W 55.
+// Tiles of 64 columns: no V by expert (512 x 3200, 5 experts, M = 6449 W 19.3, V 20.5; with 1024 x 4096 W 37, V 36), and U by two waves of
+// 32 x 32 while they are few and their lists short (640 x 270, half, M = 4735 4.3 against 4.6; 2048 x 1024, 8 experts, M = 2048, 16
+// steps 7.6 against 7.1).
 template <int GB>
 static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
   const int64_t M = g.M, n = ((int64_t)g.n_tiles * GB + 3) / 4;        // column tiles of 128
   const int steps = g.list_len / 2;
-  enum { R, Q, P, W, U, S, S2 } shape;
-  if (g.offsets && M / g.n_members < 2048) {
-    const int64_t met = g.n_members < M ? g.n_members : M;
-    shape = (M / 32 + met) * n * 4 <= 1024 ? S : (M / 64 + met) * n < 512 ? U : W;
+  enum { R, Q, P, V, W, U, S, S2 } shape;
+  int64_t tiles32;
+  if (g.offsets && M / g.n_members < 4096) {
+    const int64_t met = g.n_members < M ? g.n_members : M, tiles64 = (M / 64 + met) * n;
+    tiles32 = (M / 32 + met) * n;
+    if (tiles32 * 4 <= 1024) shape = S;
+    else if (GB == 4 && tiles64 >= 1300) shape = V;
+    else shape = tiles64 >= 640 && M / g.n_members >= 192 ? W : U;
   } else {
     auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
-    if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles(32) * 4 <= 256 ? S : S2;
-    else if (tiles(256) >= 384) shape = steps >= (tiles(256) > 512 ? 16 : 32) ? R : Q;
-    else shape = tiles(128) >= 200 ? P : U;
+    tiles32 = tiles(32);
+    if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles32 * 4 <= 256 ? S : S2;
+    else if (tiles(256) >= 384 && steps >= (tiles(256) > 512 ? 16 : 32)) shape = R;
+    else if (tiles(256) > (GB == 4 ? 768 : 512)) shape = Q;
+    else if (tiles(64) >= 1200) shape = V;
+    else if (steps >= 16 && tiles(128) >= 200 && tiles(128) <= 256) shape = P;
+    else shape = tiles(64) >= 640 ? W : U;
   }
   if (shape == S) return launch_mx4<GB, 1, 1, 1, 1, 4, 4>(g, stream);
   if (shape == S2) return launch_mx4<GB, 1, 1, 2, 1, 4, 4>(g, stream);
+  if (GB == 2 && shape == U && tiles32 <= 600 && steps <= 12) return launch_mx4<2, 1, 1, 1, 2, 1, 4>(g, stream);
+  if (shape == U) return launch_mx4<GB, 1, 2, 1, 1, 1, 4>(g, stream);
+  if (shape == W) return launch_mx4<GB, 2, 2, 1, 1, 1, GB == 4 ? 2 : 3>(g, stream);
   if constexpr (GB == 4) {
     if (shape == R) return launch_mx4<4, 4, 4, 4, 1, 1, 3>(g, stream);
     if (shape == Q) return launch_mx4<4, 2, 4, 4, 1, 1, 2>(g, stream);
     if (shape == P) return launch_mx4<4, 2, 2, 2, 2, 1, 4>(g, stream);
-    if (shape == W) return launch_mx4<4, 2, 2, 1, 2, 1, 3>(g, stream);
-    return launch_mx4<4, 1, 2, 1, 2, 1, 4>(g, stream);
-  } else {      // tiles of 64 columns: R and Q 512 x 64 (4 waves), P 256 x 64 (4), W 64 x 64 (1), U 32 x 64 (2)
+    return launch_mx4<4, 2, 4, 1, 1, 1, 2>(g, stream);
+  } else {      // tiles of 64 columns: R and Q 512 x 64 (4 waves), P 256 x 64 (4), V 128 x 64 (1)
     if (shape == R || shape == Q) return launch_mx4<2, 4, 2, 4, 1, 1, 2>(g, stream);
     if (shape == P) return launch_mx4<2, 2, 2, 4, 1, 1, 4>(g, stream);
-    if (shape == W) return launch_mx4<2, 2, 2, 1, 1, 1, 4>(g, stream);
-    return launch_mx4<2, 1, 1, 1, 2, 1, 4>(g, stream);
+    return launch_mx4<2, 4, 2, 1, 1, 1, 2>(g, stream);
   }
 }
 

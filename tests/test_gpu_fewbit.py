@@ -390,9 +390,9 @@ def test_gemm_mx4(M, K, N, G, mask):
 
 
 @pytest.mark.parametrize("G", [64, 128])
-@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (3001, 700, 1290), (600, 2000, 900)])
+@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (8199, 300, 3200), (3001, 700, 1290), (600, 2000, 900)])
 def test_gemm_mx4_of_many_tokens(M, K, N, G):
-    """The tile shapes of larger products: 512 and 256 rows, with long and short lists, 128 rows, lists shared among waves."""
+    """The tile shapes of larger products: 512, 256 and 64 rows, with long and short lists, 128 rows, lists shared among waves."""
     rng = np.random.default_rng(M + K)
     m = block_mask(rng, K, N, G, 1.0, 0.95)
     B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
@@ -473,8 +473,11 @@ def _grouped(h, Q, S, M, N, off, ldc=None):
     (96, 130, 128, np.cumsum([0] + list(range(1, 18)) + list(range(70, 78))).tolist()),
     (96, 130, 64, [3] + [12 + 8 * i for i in range(9)] + [141]),
     (200, 600, 128, [0, 1500, 1511, 4000, 4063, 5000, 6200, 7000, 7995]),
+    (100, 1500, 64, [0, 1500, 1511, 4000, 4063, 5000, 6200, 7000, 7995]),
+    (100, 1500, 128, [0, 1500, 1511, 4000, 4063, 5000, 6200, 7000, 7995]),
     (1030, 2100, 128, [5, 4000, 8190]),
-    (500, 1500, 64, [5, 4100, 8190]),
+    (500, 1500, 64, [5, 4100, 8390]),
+    (1030, 2100, 128, [7, 8300]),
     (128, 128, 128, [0] + sorted(np.random.default_rng(1).integers(0, 400, 79).tolist()) + [400]),
 ])
 def test_grouped(K, N, G, off):
