@@ -331,12 +331,13 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 //   S  32 x 32 (4 on shares of the list)   S2 64 x 32 (2 x 4)
 // R for long lists: 4096 x 4096, all, M = 8192 R 77, Q 95; half, R 46, Q 55; M = 4096 R 25.7, Q 28.6, V 28.4; M = 3100 24.8, 25.0, 24.3;
 // 1024 x 4096, all (16 steps), M = 8192 R 34.4, Q 35.5, M = 4096 16.8, 16.4; half (8 steps) 26.6, 24.6 and 14.8, 13.4; 8192 cubed
-// R 263.  Else up to about a round and a half of 256 rows V, above Q: 1024 x 4096, half, M = 3100 V 12.3, Q 12.7, M = 6000 22.9,
-// 23.6, M = 8192 27.2, 25.5; 2048 x 2048, half, M = 6000 V 14.3, Q 16.2, P 15.2.  Of the small ones by how many there are (a
-// CU takes four to five waves of W in the time of two or three larger tiles): 4096 x 4096, half, M = 2500 V 21.3, W 22.6, M = 2048 V
-// 16.7, W 16.7, U 22.8, M = 1536 V 15.9, W 14.3, U 17.7; 1024 x 1024, half, M = 10000 V 10.1, W 10.0, U 10.8, M = 5000 W 7.5, U
-// 7.4, M = 3300 W 6.7, U 5.9, P 6.4.  One round of P, long lists: 4096 x 4096, half, M = 1024 P 11.3, W 12.6, U 13.1, 4096 x 2048, M =
-// 1700 10.5, 12.4, 10.8; short ones 1024 x 4096, M = 1024 6.9, 7.2, 6.8.
+// R 263.  Else by rounds: a CU holds 12 waves of W (1536 tiles of 64 x 128), 8 of V or 2 workgroups of Q (2048).  1024 x 4096, half, a
+// tenth of the columns pruned: M = 3100 (1421 tiles) W 12.1, V 12.7, Q 12.9; M = 4096 (1856) 15.0, 13.6, 13.3; M = 5000 (2291) 20.1,
+// 20.2, 19.8; M = 6000 (2726) 27.8, 23.8, 21.9; a quarter, M = 5000 14.3, 16.4, 16.3; 768 x 3000, half, M = 6000 (2068) 14.0, 17.3,
+// 17.7, M = 7000 (2420) 16.6, 18.5, 18.1, M = 8192 (2816) 21.8, 20.7, 20.9.  Long lists, few tiles: 4096 x 4096, half, M = 2500 V
+// 21.3, W 22.6, a quarter, M = 3100 15.8, 16.1.  Small ones: 1024 x 1024, half, M = 5000 (632) W 7.5, U 7.4, M = 3300 W 6.7, U 5.9,
+// P 6.4; 4096 x 4096, half, M = 1536 (768) W 14.3, U 17.7, P 16.3.  One round of P, long lists: 4096 x 4096, half, M = 1024 P 11.3, W
+// 12.6, U 13.1, 4096 x 2048, M = 1700 10.5, 12.4, 10.8; short ones 1024 x 4096, M = 1024 6.9, 7.2, 6.8.
 // Lists shared among waves where tiles of 64 rows would be fewer than 160 and a list is long: 4096 x 4096, half, M = 128
 // S2 5.2, S 6.0, U 7.6; all, M = 256 S2 10.5, U 12.0; 4096 x 1024, all, M = 512 S2 6.9, U 10; up to 256 tiles of S it has
 // the shortest way: 1024 x 1024, half, M = 256 S 3.0, S2 3.1, U 3.4; 4096 x 4096, M = 1 S 3.7, S2 4.3.
@@ -357,15 +358,15 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
     const int64_t met = g.n_members < M ? g.n_members : M, tiles64 = (M / 64 + met) * n;
     tiles32 = (M / 32 + met) * n;
     if (tiles32 * 4 <= 1024) shape = S;
-    else if (GB == 4 && tiles64 >= 1300) shape = V;
+    else if (GB == 4 && (tiles64 > 1536 || (tiles64 >= 1200 && steps >= 16))) shape = V;
     else shape = tiles64 >= 640 && M / g.n_members >= 192 ? W : U;
   } else {
     auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
     tiles32 = tiles(32);
     if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles32 * 4 <= 256 ? S : S2;
     else if (tiles(256) >= 384 && steps >= (tiles(256) > 512 ? 16 : 32)) shape = R;
-    else if (tiles(256) > (GB == 4 ? 768 : 512)) shape = Q;
-    else if (tiles(64) >= 1200) shape = V;
+    else if (tiles(64) > 2450 || (tiles(64) > 1536 && (tiles(64) <= 2048 || steps >= 16))) shape = Q;
+    else if (tiles(64) >= 1200 && steps >= 16) shape = V;
     else if (steps >= 16 && tiles(128) >= 200 && tiles(128) <= 256) shape = P;
     else shape = tiles(64) >= 640 ? W : U;
   }

@@ -390,9 +390,10 @@ def test_gemm_mx4(M, K, N, G, mask):
 
 
 @pytest.mark.parametrize("G", [64, 128])
-@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (8199, 300, 3200), (3001, 700, 1290), (600, 2000, 900)])
+@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (8199, 300, 3200), (3001, 700, 1290), (600, 2000, 900),
+                                   (5000, 1030, 2000), (5000, 300, 1300), (1700, 1030, 2000)])
 def test_gemm_mx4_of_many_tokens(M, K, N, G):
-    """The tile shapes of larger products: 512, 256 and 64 rows, with long and short lists, 128 rows, lists shared among waves."""
+    """The tile shapes of larger products: 512 and 256 rows, 128 rows, tiles of single waves, lists shared among waves."""
     rng = np.random.default_rng(M + K)
     m = block_mask(rng, K, N, G, 1.0, 0.95)
     B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
