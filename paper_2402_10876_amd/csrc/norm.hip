@@ -357,15 +357,26 @@ hipError_t run_norm(const NormArgs& g, hipStream_t stream) {
 }
 
 // ---- long tokens in slices of their rows ----------------------------------------------------------
-// A workgroup that owns whole tokens reads and writes narrow pieces of rows (64 and 32 bytes, of lines of 128).  With many rows
-// three launches on 128 tokens x one slice of the rows are faster, every access whole lines: sums of the slices (and H), sums of
-// the tokens, outputs.  No memory beyond the outputs is used: between the launches the sums of a slice, 8 bytes per token, lie in
-// the first rows of that slice of Q (8 rows of bytes; of Y 4 rows of halves without Q), which the last launch reads before it
-// writes them.  us, one launch / three (residual, int8 output, from HBM): 4096
-// rows, 1024 tokens 26 / 20, 4096 tokens 49 / 42, 8192 tokens 79 / 68, with both outputs 105 / 85; 8192 rows, 1024 tokens 52 / 28,
-// 8192 tokens 167 / 128; 2048 rows, 4096 tokens 25 / 27, 8192 tokens 41 / 43; 4096 rows, 512 tokens 18 / 19, without a
-// residual, 8192 tokens 39 / 47.
-constexpr int SL_TOK = 128, SL_NT = 256, SL_RPP = SL_NT / (SL_TOK / 8), SL_CH = 8;      // 16 rows at a time, 8 times
+// A workgroup that owns whole tokens reads and writes narrow pieces of rows (64 and 32 bytes, of lines of 128), and few tokens are
+// few workgroups.  With long tokens three launches on 128 tokens x one slice of the rows are faster, every access whole lines: sums of
+// the slices (and H), sums of the tokens, outputs.  No memory beyond the outputs is used: between the launches the sums of a slice,
+// 8 bytes per token, lie in the first rows of that slice of Q (8 rows of bytes; of Y 4 rows of halves without Q), which the last
+// launch reads before it writes them.  us, one launch / three, from HBM, residual and int8 output: 4096 rows, 32 tokens 9.8 / 10.5, 64
+// tokens 14.7 / 10.7, 512 tokens 17.7 / 13.2, 8192 tokens 79 / 65.6; 2500 rows, 64 tokens 10.8 / 10.8, 1024 tokens 14.0 / 13.7; 8192
+// rows, 16 tokens 12.0 / 12.2, 256 tokens 32 / 14.5; 16384 rows, 8 tokens 68 / 16; 2048 rows, 1024 tokens 11.8 / 12.8, 8192 tokens
+// 40.8 / 36.8; 1024 rows, 8192 tokens 20.9 / 24.5, 16384 tokens 38.2 / 36.7.  Without a residual: 4096 rows, 8192 tokens 41.8 / 42.9,
+// with both outputs 62.7 / 55.4; 6000 rows, 64 tokens 11.5 / 11.6, 8192 tokens 60.7 / 59.8; 8192 rows, 64 tokens 14.5 / 12.0, 8192
+// tokens 88 / 76.  (Of 8 rows a lane in workgroups of 256 threads 72 where 2 rows in 1024 threads take 65.6.)
+constexpr int SL_TOK = 128, SL_NT = 1024, SL_RPP = SL_NT / (SL_TOK / 8), SL_CH = 2;      // 64 rows at a time, twice
+constexpr int SL_ROWS = SL_CH * SL_RPP;
+
+static bool slices_pay(const NormArgs& g) {
+  const int64_t values = (int64_t)g.M * g.K;
+  if ((((int64_t)g.M + SL_TOK - 1) / SL_TOK) * ((g.K + SL_ROWS - 1) / SL_ROWS) * SL_NT > 0xffffffffll) return false;      // threads of a grid
+  if (g.K > 8192) return true;
+  if (g.R) return g.K > 2048 ? values >= 160000 : g.K >= 1024 && values >= 1 << 24;
+  return g.K > 4096 ? values >= 400000 : g.K > 2048 && g.Y && g.Q && values >= 1 << 24;
+}
 
 __device__ __forceinline__ int slice_row(const NormArgs& g, int s, int n) { return (int)((int64_t)g.K * s / n); }
 
@@ -422,7 +433,8 @@ struct SliceLane {
 };
 
 __global__ __launch_bounds__(SL_NT) void norm_slices_kernel(NormArgs g, int n) {
-  __shared__ float s_sum[4][SL_TOK], s_top[4][SL_TOK];
+  constexpr int NW = SL_NT / 64;
+  __shared__ float s_sum[NW][SL_TOK], s_top[NW][SL_TOK];
   const SliceLane a(g, n);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   half8 h[SL_CH];
@@ -474,16 +486,19 @@ __global__ __launch_bounds__(SL_NT) void norm_slices_kernel(NormArgs g, int n) {
   }
   __syncthreads();
   if (tid < SL_TOK && a.m0 + tid < g.M) {
-    const float x = s_sum[0][tid] + s_sum[1][tid] + s_sum[2][tid] + s_sum[3][tid];
-    float t = s_top[0][tid];
+    float x = s_sum[0][tid], t = s_top[0][tid];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) t = __builtin_fmaxf(t, s_top[w][tid]);
+    for (int w = 1; w < NW; ++w) {
+      x += s_sum[w][tid];
+      t = __builtin_fmaxf(t, s_top[w][tid]);
+    }
     put_sums(g, a.k0, a.m0 + tid, make_uint2(__float_as_uint(x), x < __builtin_inff() ? __float_as_uint(t) : INF_BITS));
   }
 }
 
-// 16 tokens, 16 groups of threads on the slices by turns: up to 32 slices (4096 rows) in one round trip.
-constexpr int TK_TOK = 16, TK_GRP = 16;
+// TK_TOK tokens, 16 groups of threads on the slices by turns: up to 32 slices (4096 rows) in one round trip.
+constexpr int TK_GRP = 16;
+template <bool NORM, int TK_TOK>
 __global__ __launch_bounds__(TK_TOK * TK_GRP) void norm_tokens_kernel(NormArgs g, int n) {
   __shared__ float s_sum[TK_GRP][TK_TOK];
   __shared__ uint32_t s_top[TK_GRP][TK_TOK];
@@ -512,7 +527,7 @@ __global__ __launch_bounds__(TK_TOK * TK_GRP) void norm_tokens_kernel(NormArgs g
       sum += s_sum[w][tok];
       top = max(top, s_top[w][tok]);
     }
-    const Token t = finish_token<true>(sum, top, g);
+    const Token t = finish_token<NORM>(sum, top, g);
     if (g.scale && m < g.M) g.scale[m] = t.scale;
     s_out[tok] = make_uint2(__float_as_uint(t.inv), top);
   }
@@ -576,11 +591,15 @@ __global__ __launch_bounds__(SL_NT) void norm_outputs_kernel(NormArgs g, int n) 
   }
 }
 
-// n slices of at most 128 and at least 8 rows.
+// n slices of at most SL_ROWS and at least 8 rows.  (The quantiser is the norm's first and last launch without R and gamma.)
+template <bool NORM>
 hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
   const unsigned bands = (unsigned)(((int64_t)g.M + SL_TOK - 1) / SL_TOK);
   hipError_t e = launch_kernel(norm_slices_kernel, dim3(bands * n), dim3(SL_NT), stream, g, n);
-  if (e == hipSuccess) e = launch_kernel(norm_tokens_kernel, dim3((unsigned)(((int64_t)g.M + TK_TOK - 1) / TK_TOK)), dim3(TK_TOK * TK_GRP), stream, g, n);
+  // (64 tokens: 8192 x 4096 66.9 -> 65.6 us; 8192 x 128 13.9 -> 14.5)
+  if (e == hipSuccess)
+    e = g.M > 2048 ? launch_kernel(norm_tokens_kernel<NORM, 64>, dim3((unsigned)(((int64_t)g.M + 63) / 64)), dim3(64 * TK_GRP), stream, g, n)
+                   : launch_kernel(norm_tokens_kernel<NORM, 32>, dim3((unsigned)((g.M + 31) / 32)), dim3(32 * TK_GRP), stream, g, n);
   if (e == hipSuccess) e = launch_kernel(norm_outputs_kernel, dim3(bands * n), dim3(SL_NT), stream, g, n);
   return e;
 }
@@ -595,7 +614,7 @@ hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
 template <bool NORM>
 static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   const int K = g.K;
-  if (NORM && g.R && K > 2048 && (int64_t)g.M * K >= 3 << 20) return run_norm_slices(g, (K + SL_CH * SL_RPP - 1) / (SL_CH * SL_RPP), stream);
+  if (slices_pay(g)) return run_norm_slices<NORM>(g, (K + SL_ROWS - 1) / SL_ROWS, stream);
   if (g.M <= 2048 && K <= 8192) {
     if (K <= 1024) return run_norm<NORM, 8, 512, 2>(g, stream);
     if (K <= 2048) return run_norm<NORM, 8, 512, 4>(g, stream);

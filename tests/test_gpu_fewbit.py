@@ -83,7 +83,7 @@ def test_norm_of_any_number_of_tokens(M):
 
 
 @pytest.mark.parametrize("M,K", [(2049, 64), (2500, 1100), (2200, 2100), (4097, 40), (4100, 1030), (4098, 2050), (8200, 300),
-                                 (16321, 2049), (16500, 2049), (16450, 96)])
+                                 (16321, 2049), (16500, 2049), (16450, 96), (8203, 2060), (16397, 1030), (1030, 4200)])
 def test_norm_and_quantiser_of_many_tokens(M, K):
     """Every number of tokens per workgroup, with a ragged last one."""
     import torch
@@ -101,7 +101,17 @@ def test_norm_and_quantiser_of_many_tokens(M, K):
     assert np.array_equal(np.isnan(s), np.isnan(scale)) and (np.abs(np.nan_to_num(s - scale)) <= 2.0 ** -23 * np.nan_to_num(scale)).all()
 
 
-@pytest.mark.parametrize("M,K", [(1537, 2049), (1001, 3333), (768, 4096), (400, 8200)])
+@pytest.mark.parametrize("M,K", [(1, 8193), (19, 8195), (3, 131071), (130, 10000)])
+def test_norm_of_few_very_long_tokens(M, K):
+    print(f"few long tokens M={M} K={K}", flush=True)
+    X, R = acts(M + K, M, K), acts(M + K + 1, M, K, 3.0)
+    _check_norm(X, R, None, 1e-5, i8=True, f16=True)
+    _check_norm(X, None, None, 1e-5, i8=False, f16=True)
+    X[M - 1, K - 1] = np.nan
+    _check_norm(X, None, None, 1e-5, i8=True, f16=False)
+
+
+@pytest.mark.parametrize("M,K", [(1537, 2049), (1001, 3333), (768, 4096), (400, 8200), (79, 2050), (2051, 2500)])
 def test_norm_of_long_tokens_in_slices(M, K):
     """With a residual and many rows the work is cut along the rows: every combination of outputs, in place, infinities."""
     print(f"slices M={M} K={K}", flush=True)
@@ -163,7 +173,7 @@ def test_norm_largest_and_smallest_values():
     _check_norm(X, None, None, 1e-30, i8=True, f16=True)
 
 
-@pytest.mark.parametrize("M,K", [(1, 1), (5, 31), (40, 768), (33, 1003), (64, 4100)])
+@pytest.mark.parametrize("M,K", [(1, 1), (5, 31), (40, 768), (33, 1003), (64, 4100), (101, 4200), (1, 8193), (5, 20000)])
 def test_quant_i8(M, K):
     import torch
     X = acts(M * 3 + K, M, K)
