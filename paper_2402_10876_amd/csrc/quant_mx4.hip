@@ -5,8 +5,11 @@
 // past 6 to 6; checked for every fp16 value against the definition).  Bound by memory: 2 bytes in and 17/32 out per value.
 //   K x M : a lane takes two neighbouring tokens, 32 loads of 4 bytes, all under way at once; a wave reads 256 bytes of
 //           each row and writes 2 KiB of codes in a run.
-//   M x K : a wave takes 16 blocks of 8 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
-//           collected in LDS so that the writes are whole lines (8 tokens of a block row) as well.
+//   M x K : a wave takes 16 blocks of 4 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
+//           collected in LDS so that the writes are runs of 64 bytes (4 tokens of a block row).  Workgroups that start
+//           together read whole tokens: side by side down the rows they meet the same channels of memory where a row
+//           is a power of two of bytes.  us, tokens first / whole tokens: 8192 x 4096 19.8 / 17.3 (floor 16.5), 8192 x 2048 10.3 /
+//           8.1, 4096 x 768 3.7 / 3.6; of 8 tokens 20.9 / 18.0, and one token of 4096 values 2.7 against 2.35.
 #include <type_traits>
 
 #include "device_common.h"
@@ -57,11 +60,14 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
 
 }  // namespace
 
-// K x M.  One wave: 128 tokens x one block of rows.
-__global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n_blocks) {
+// K x M.  One wave: 128 tokens x one block of rows; neighbouring workgroups along the rows (n_rows of them) or along the tokens.
+// us along rows / tokens: 4096 x 768 3.5 / 3.9, 1957 x 1003 3.0 / 3.4, 5000 x 1003 4.7 / 5.2, 8192 x 1024 5.5 / 5.5, 8192 x 4096 20.7 / 20.0.
+__global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n_blocks, int n_rows, int n_tokens) {
   const int lane = threadIdx.x & 63;
-  const int b = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = ((int)blockIdx.x * 64 + lane) * 2;
+  const int bid = (int)blockIdx.x;
+  const int at_rows = n_rows ? bid % n_rows : bid / n_tokens, at_tokens = n_rows ? bid / n_rows : bid % n_tokens;
+  const int b = at_rows * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = (at_tokens * 64 + lane) * 2;
   if (b >= n_blocks || m >= g.M) return;
   const int k0 = b * MX4_BLOCK, rows = min(g.K - k0, MX4_BLOCK);
   const _Float16* x = g.X + (size_t)k0 * g.ldx + m;
@@ -92,11 +98,12 @@ __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n
 }
 
 // M x K.  One wave: TOK tokens x 16 blocks; four lanes hold a block of a token.
-template <int TOK>
-__global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks) {
+constexpr int TOK = 4;
+__global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks, int n_cols) {
   __shared__ __attribute__((aligned(16))) uint32_t codes[4][16 * TOK * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = ((int)blockIdx.x * 4 + wave) * TOK, b0 = (int)blockIdx.y * 16;
+  const int at_tokens = (int)blockIdx.x / n_cols, at_cols = (int)blockIdx.x - at_tokens * n_cols;
+  const int m0 = (at_tokens * 4 + wave) * TOK, b0 = at_cols * 16;
   if (m0 >= g.M) return;
   const int k = b0 * MX4_BLOCK + lane * 8, left = g.K - k;         // values of the lane in front of K: left and more
   const _Float16* x = g.X + (size_t)m0 * g.ldx + (left > 0 ? k : 0);
@@ -150,9 +157,14 @@ __global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n
 
 hipError_t launch_quant_mx4(bool km, const QuantMx4Args& g, hipStream_t stream) {
   const int nb = (g.K + MX4_BLOCK - 1) / MX4_BLOCK;
-  if (km)
-    return launch_kernel(quant_mx4_km_kernel, dim3((unsigned)(((int64_t)g.M + 127) / 128), (nb + 3) / 4), dim3(256), stream, g, nb);
-  return launch_kernel(quant_mx4_mk_kernel<8>, dim3((unsigned)(((int64_t)g.M + 31) / 32), (nb + 15) / 16), dim3(256), stream, g, nb);
+  const int64_t per = km ? 128 : 4 * TOK, n_tokens = (g.M + per - 1) / per, n_other = km ? (nb + 3) / 4 : (nb + 15) / 16;
+  if (n_tokens * n_other * 256 > 0xffffffffll) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(n_tokens * n_other));
+  if (km) {
+    const bool along_rows = (int64_t)g.M * g.K < 8 << 20;
+    return launch_kernel(quant_mx4_km_kernel, grid, dim3(256), stream, g, nb, along_rows ? (int)n_other : 0, (int)n_tokens);
+  }
+  return launch_kernel(quant_mx4_mk_kernel, grid, dim3(256), stream, g, nb, (int)n_other);
 }
 
 }  // namespace twg

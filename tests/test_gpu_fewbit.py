@@ -332,7 +332,7 @@ def _same_codes(Q, S, X, ldq):
 
 
 @pytest.mark.parametrize("layout", ["KM", "MK"])
-@pytest.mark.parametrize("M,K", [(1, 1), (1, 32), (2, 31), (33, 33), (130, 300), (64, 1003), (257, 64)])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 32), (2, 31), (33, 33), (130, 300), (64, 1003), (257, 64), (19, 2100), (8203, 1030)])
 def test_quant_mx4(M, K, layout):
     X = acts(M + K, M, K)
     if M > 4:
