@@ -4,7 +4,8 @@
 // the magnitudes do, infinities and NaN on top), v_cvt_scalef32_pk_fp4_f16 rounds two values at a time (nearest even,
 // past 6 to 6; checked for every fp16 value against the definition).  Bound by memory: 2 bytes in and 17/32 out per value.
 //   K x M : a lane takes two neighbouring tokens, 32 loads of 4 bytes, all under way at once; a wave reads 256 bytes of
-//           each row and writes 2 KiB of codes in a run.
+//           each row and writes 2 KiB of codes in a run.  With few values a lane takes 4 rows, so that there are lanes at work and
+//           no lane has 32 loads to issue.
 //   M x K : a wave takes 16 blocks of 4 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
 //           collected in LDS so that the writes are runs of 64 bytes (4 tokens of a block row).  Workgroups that start
 //           together read whole tokens: side by side down the rows they meet the same channels of memory where a row
@@ -97,6 +98,44 @@ __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n
   }
 }
 
+// K x M, few values.  One wave: 16 tokens x one block of rows; a lane takes two tokens and 4 rows.  us, 32 rows a lane / 4 rows: 1 x
+// 4096 3.7 / 2.2, 16 x 4096 4.2 / 2.3, 128 x 1024 2.9 / 2.3, 1024 x 1024 3.0 / 2.6, 2048 x 1024 3.1 / 2.9, 4096 x 768 3.6 / 6.0.
+__global__ __launch_bounds__(256) void quant_mx4_few_kernel(QuantMx4Args g, int n_blocks, int n_rows) {
+  const int lane = threadIdx.x & 63, pair = lane & 7, part = lane >> 3;
+  const int at_tokens = (int)blockIdx.x / n_rows, at_rows = (int)blockIdx.x - at_tokens * n_rows;
+  const int b = at_rows * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = at_tokens * 16 + pair * 2, k = b * MX4_BLOCK + part * 4;
+  if (b >= n_blocks) return;
+  const _Float16* x = g.X + (m < g.M ? m : 0);
+  uint32_t v[4], top = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t*)(x + (size_t)min(k + j, g.K - 1) * g.ldx);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (k + j >= g.K) v[j] = 0;
+    top = max_u16x2(top, v[j] & 0x7fff7fffu);
+  }
+  top = max_u16x2(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x128, 0xf, 0xf, true));      // row_ror:8
+  const auto t16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+  top = max_u16x2(t16[0], t16[1]);
+  const auto t32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+  top = max_u16x2(t32[0], t32[1]);
+  if (m >= g.M) return;
+  const size_t at = (size_t)b * g.ldq + m;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    if (m + t >= g.M) break;
+    const uint32_t sel = t ? 0x07060302u : 0x05040100u, s = scale_byte(t ? top >> 16 : top & 0xffffu);
+    const float f = __uint_as_float((s == MX4_NAN ? MX4_ONE : s) << 23);
+    const uint32_t lo = __builtin_amdgcn_perm(v[1], v[0], sel), hi = __builtin_amdgcn_perm(v[3], v[2], sel);
+    uint32_t o = 0;
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, lo), f, 0);
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(o, __builtin_bit_cast(half2v, hi), f, 1);
+    *(uint16_t*)(g.Q + (at + t) * 16 + part * 2) = s == MX4_NAN ? 0 : (uint16_t)o;
+    if (part == 0) g.S[at + t] = (uint8_t)s;
+  }
+}
+
 // M x K.  One wave: TOK tokens x 16 blocks; four lanes hold a block of a token.
 constexpr int TOK = 4;
 __global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks, int n_cols) {
@@ -157,13 +196,14 @@ __global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n
 
 hipError_t launch_quant_mx4(bool km, const QuantMx4Args& g, hipStream_t stream) {
   const int nb = (g.K + MX4_BLOCK - 1) / MX4_BLOCK;
-  const int64_t per = km ? 128 : 4 * TOK, n_tokens = (g.M + per - 1) / per, n_other = km ? (nb + 3) / 4 : (nb + 15) / 16;
+  const int64_t values = (int64_t)g.M * g.K;
+  const bool few = km && values <= 1 << 21;
+  const int64_t per = few ? 16 : km ? 128 : 4 * TOK;
+  const int64_t n_tokens = (g.M + per - 1) / per, n_other = km ? (nb + 3) / 4 : (nb + 15) / 16;
   if (n_tokens * n_other * 256 > 0xffffffffll) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(n_tokens * n_other));
-  if (km) {
-    const bool along_rows = (int64_t)g.M * g.K < 8 << 20;
-    return launch_kernel(quant_mx4_km_kernel, grid, dim3(256), stream, g, nb, along_rows ? (int)n_other : 0, (int)n_tokens);
-  }
+  if (few) return launch_kernel(quant_mx4_few_kernel, grid, dim3(256), stream, g, nb, (int)n_other);
+  if (km) return launch_kernel(quant_mx4_km_kernel, grid, dim3(256), stream, g, nb, values < 8 << 20 ? (int)n_other : 0, (int)n_tokens);
   return launch_kernel(quant_mx4_mk_kernel, grid, dim3(256), stream, g, nb, (int)n_other);
 }
 

@@ -332,7 +332,8 @@ def _same_codes(Q, S, X, ldq):
 
 
 @pytest.mark.parametrize("layout", ["KM", "MK"])
-@pytest.mark.parametrize("M,K", [(1, 1), (1, 32), (2, 31), (33, 33), (130, 300), (64, 1003), (257, 64), (19, 2100), (8203, 1030)])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 32), (2, 31), (33, 33), (130, 300), (64, 1003), (257, 64), (19, 2100), (5003, 700),
+                                 (8203, 1030)] + [(M, 77) for M in range(3, 18)])
 def test_quant_mx4(M, K, layout):
     X = acts(M + K, M, K)
     if M > 4:
@@ -356,6 +357,9 @@ def test_quant_mx4_every_value():
     for layout in (tw.LAYOUT_KM, tw.LAYOUT_MK):
         Q, S = fu.quant_mx4_dev(tw, X, layout, _stream())
         _same_codes(Q, S, X, None)
+    X = np.ascontiguousarray(np.concatenate([X, X[:, ::-1], -X], 1))          # (more values than the kernel for few takes)
+    Q, S = fu.quant_mx4_dev(tw, X, tw.LAYOUT_KM, _stream())
+    _same_codes(Q, S, X, None)
 
 
 def _gemm_mx4(p, Q, S, M, N, ldc=None):
