@@ -404,10 +404,10 @@ def test_gemm_mx4(M, K, N, G, mask):
 
 
 @pytest.mark.parametrize("G", [64, 128])
-@pytest.mark.parametrize("M,K,N", [(8199, 1030, 2100), (8199, 500, 1500), (8199, 300, 3200), (3001, 700, 1290), (600, 2000, 900),
+@pytest.mark.parametrize("M,K,N", [(20, 3000, 300), (5, 1500, 300), (33, 700, 200), (8199, 1030, 2100), (8199, 500, 1500), (8199, 300, 3200), (3001, 700, 1290), (600, 2000, 900),
                                    (5000, 1030, 2000), (5000, 300, 1300), (1700, 1030, 2000)])
-def test_gemm_mx4_of_many_tokens(M, K, N, G):
-    """The tile shapes of larger products: 512 and 256 rows, 128 rows, tiles of single waves, lists shared among waves."""
+def test_gemm_mx4_of_every_shape(M, K, N, G):
+    """Lists of every length for few tokens and the tile shapes of larger products: 512 and 256 rows, 128 rows, tiles of single waves, lists shared among waves."""
     rng = np.random.default_rng(M + K)
     m = block_mask(rng, K, N, G, 1.0, 0.95)
     B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
