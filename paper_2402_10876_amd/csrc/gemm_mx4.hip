@@ -342,7 +342,7 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 // S2 5.2, S 6.0, U 7.6; all, M = 256 S2 10.5, U 12.0; 4096 x 1024, all, M = 512 S2 6.9, U 10; up to 256 tiles of S it has
 // the shortest way: 1024 x 1024, half, M = 256 S 3.0, S2 3.1, U 3.4; 4096 x 4096, M = 1 S 3.7, S2 4.3.  Shares of S: two, four
 // with 4 steps under way, four with 8: 1024 x 4096, half (8 steps), M = 1 3.0, 3.2, 3.5; 1024 x 1024, 16 experts, M = 64 4.5, 4.8, 5.5;
-// 2048 x 1024, 8 experts (16 steps), M = 256 5.1, 5.3, 5.9; 4096 x 4096, half (32), M = 32 4.1, 3.75, 3.6, all (64) 6.4, 5.4, 4.8.
+// 2048 x 1024, 8 experts (16 steps), M = 256 5.1, 5.3, 5.9; 1536 x 672, half (about 14), M = 359 3.8, 3.6; 4096 x 4096, half (32), M = 32 4.1, 3.75, 3.6, all (64) 6.4, 5.4, 4.8.
 // By expert, where ranges end inside tiles (half kept): 2048 x 1024, 8 experts, M = 8192 W 13.1, V 14.4, U 15.2, Q 16.7, M = 6000 W
 // 11.2, U 12.1, M = 2048 U 7.2, W 8.3, M = 512 S 5.7, U 6.2; 1024 x 1024, 8 experts, M = 12000 V 12.7, W 13.7; 1024 x 4096, 8 experts,
 // M = 8192 V 33, W 37, Q 34; 4096 x 2048, 16 experts, M = 5000 V 32, W 39.  Few tokens each: 1024 x 1024, 32 experts, M = 4000 U 9.0, W
@@ -373,7 +373,7 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
     else shape = tiles(64) >= 640 ? W : U;
   }
   if (shape == S) {
-    if (steps <= 16) return launch_mx4<GB, 1, 1, 1, 1, 2, 4>(g, stream);
+    if (steps <= 12) return launch_mx4<GB, 1, 1, 1, 1, 2, 4>(g, stream);
     return steps <= 32 ? launch_mx4<GB, 1, 1, 1, 1, 4, 4>(g, stream) : launch_mx4<GB, 1, 1, 1, 1, 4, 8>(g, stream);
   }
   if (shape == S2) return launch_mx4<GB, 1, 1, 2, 1, 4, 4>(g, stream);
