@@ -202,7 +202,8 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
   };
 
   // Norm: sums of squares and the largest |g|, as fp32; an infinity or NaN among the h of a token shows in its sum, one
-  // among the gamma makes every token one that is not finite.  Quantiser: the largest magnitude over the fp16 bits.
+  // among the gamma in every token's largest |g| (not in the sums: Y is the formula's, whose inv does not contain gamma).
+  // Quantiser: the largest magnitude over the fp16 bits.
   float sum[NORM ? 8 : 1], top[NORM ? 8 : 1], worst = 0.f;
   uint32_t bits[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -252,7 +253,7 @@ __global__ __launch_bounds__(NT) void norm_kernel(NormArgs g) {
   const int tok = c * 8 + 2 * (lane >> 4 & 1) + 4 * (lane >> 5);
   if constexpr (NORM) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += worst;
+    for (int e = 0; e < 8; ++e) top[e] = worst == 0.f ? top[e] : __builtin_inff();
     halve(sum, [](float x, float y) { return x + y; });
     halve(top, [](float x, float y) { return __builtin_fmaxf(x, y); });
 #pragma unroll
@@ -475,7 +476,7 @@ __global__ __launch_bounds__(SL_NT) void norm_slices_kernel(NormArgs g, int n) {
     worst = __builtin_fmaf(gm, 0.f, worst);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] += worst;
+  for (int e = 0; e < 8; ++e) top[e] = worst == 0.f ? top[e] : __builtin_inff();      // (a gamma that is not finite: every token)
   halve(sum, [](float x, float y) { return x + y; });
   halve(top, [](float x, float y) { return __builtin_fmaxf(x, y); });
   const int tok = a.c * 8 + 2 * (lane >> 4 & 1) + 4 * (lane >> 5);

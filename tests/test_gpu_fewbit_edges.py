@@ -1,0 +1,77 @@
+"""Few-bit operators at the ends of what they allow: factors of the norm that are not finite (-m gpu)."""
+import numpy as np
+import pytest
+
+import paper_2402_10876_amd as tw
+from oracle import fewbit as ofb
+from tests import fewbit_util as fu
+from tests.fewbit_util import acts, up
+
+pytestmark = pytest.mark.gpu
+
+
+def _norm(X, R, gamma, eps, i8, f16):
+    """h, y, int8 values (tokens first) and scales of one call, the columns behind M looked at."""
+    import torch
+    M, K = X.shape
+    ld, ldq = up(M, 8), up(M, 16)
+    new = lambda shape, fill, dtype: torch.full(shape, fill, dtype=dtype, device="cuda")  # noqa: E731
+    Xd, Rd = fu.dev_km(X, ld), None if R is None else fu.dev_km(R, ld)
+    gd = None if gamma is None else torch.from_numpy(gamma).cuda()
+    H = None if R is None else new((K, ld), 7.0, torch.float16)
+    Y = new((K, ld), 7.0, torch.float16) if f16 else None
+    Q = new((K, ldq), 99, torch.int8) if i8 else None
+    s = new((M,), 7.0, torch.float32) if i8 else None
+    p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    tw.tw_rmsnorm(p(Xd), p(Rd), p(gd), eps, M, K, ld, p(H), p(Y), p(Q), ldq, p(s), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    out = []
+    for t, fill in ((H, 7.0), (Y, 7.0), (Q, 99)):
+        if t is not None:
+            assert bool((t[:, M:] == fill).all())
+        out.append(None if t is None else t[:, :M].cpu().numpy().T)
+    return (*out, None if s is None else s.cpu().numpy())
+
+
+def _assert_y(got, y, K):
+    """got: fp16 output, y: fp64 definition (NaN and infinities among them): NaN and each infinity in their places, every
+    other value within the roundings of fu.norm_tol and half a step of fp16."""
+    got = got.astype(np.float64)
+    assert np.array_equal(np.isnan(got), np.isnan(y))
+    inf = np.isinf(y)
+    assert np.array_equal(got[inf], y[inf])
+    fine = np.isfinite(y)
+    assert np.isfinite(got[fine]).all()
+    err, size = np.abs(got[fine] - y[fine]), np.abs(y[fine])
+    assert (err <= size * (fu.STEP16 + fu.norm_tol(K)) * (1 + fu.STEP16) + 2.0 ** -25).all()
+
+
+# One launch that keeps its rows, one that reads them again (2050 rows of 4100 and 16400 tokens without a residual), slices.
+@pytest.mark.parametrize("M,K,residual", [(1, 1, False), (40, 5, True), (40, 1500, False), (33, 1003, True), (3000, 700, True),
+                                          (4100, 300, False), (4100, 2050, False), (16400, 2049, False), (16450, 96, True),
+                                          (70, 4200, True), (1030, 2100, True), (100, 6000, False), (3, 8200, False), (5, 8200, True)])
+@pytest.mark.parametrize("i8,f16", [(False, True), (True, True), (True, False)])
+def test_norm_with_factors_that_are_not_finite(M, K, residual, i8, f16):
+    """Every token's scale is NaN and its int8 values are 0; the fp16 output is the formula's, whose root-mean-square does
+    not contain the factors: only their own rows (and a token that is not finite itself) hold infinities and NaN."""
+    X = acts(M + K, M, K)
+    R = acts(M + K + 1, M, K, 3.0) if residual else None
+    if M > 6:
+        X[5, K // 3] = -np.inf
+    for bads in ([np.inf, -np.inf, np.nan], [np.nan], [np.inf], [-np.inf])[:4 if M * K < 1 << 22 else 1]:
+        gamma = (1 + 0.3 * np.random.default_rng(K).standard_normal(K)).astype(np.float16)
+        at = [(K // 2 + 131 * i) % K for i in range(len(bads))]
+        for k, bad in zip(at, bads):
+            gamma[k] = bad
+        print(f"norm M={M} K={K} residual={residual} i8={i8} f16={f16} gamma={bads}", flush=True)
+        h, y, q, scale = ofb.rmsnorm(X, R, gamma, 1e-5)
+        assert np.isnan(scale).all() and not q.any()
+        if M > 6 and K > 3:
+            assert np.isfinite(np.delete(np.delete(y, 5, 0), at, 1)).all()
+        H, Y, Q, s = _norm(X, R, gamma, 1e-5, i8, f16)
+        if H is not None:
+            assert np.array_equal(H.view(np.uint16), h.view(np.uint16))
+        if Y is not None:
+            _assert_y(Y, y, K)
+        if Q is not None:
+            assert not Q.any() and np.isnan(s).all()
