@@ -15,6 +15,7 @@
 
 #include "device_common.h"
 #include "fewbit.h"
+#include "grid.h"
 #include "mx4_format.h"
 
 namespace twg {
@@ -65,7 +66,7 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
 // us along rows / tokens: 4096 x 768 3.5 / 3.9, 1957 x 1003 3.0 / 3.4, 5000 x 1003 4.7 / 5.2, 8192 x 1024 5.5 / 5.5, 8192 x 4096 20.7 / 20.0.
 __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n_blocks, int n_rows, int n_tokens) {
   const int lane = threadIdx.x & 63;
-  const int bid = (int)blockIdx.x;
+  const int bid = (int)(blockIdx.y * gridDim.x + blockIdx.x);      // (those past the last one: no block or no token)
   const int at_rows = n_rows ? bid % n_rows : bid / n_tokens, at_tokens = n_rows ? bid / n_rows : bid % n_tokens;
   const int b = at_rows * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = (at_tokens * 64 + lane) * 2;
@@ -138,10 +139,11 @@ __global__ __launch_bounds__(256) void quant_mx4_few_kernel(QuantMx4Args g, int 
 
 // M x K.  One wave: TOK tokens x 16 blocks; four lanes hold a block of a token.
 constexpr int TOK = 4;
-__global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks, int n_cols) {
+__global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n_blocks, uint32_t n_cols) {
   __shared__ __attribute__((aligned(16))) uint32_t codes[4][16 * TOK * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int at_tokens = (int)blockIdx.x / n_cols, at_cols = (int)blockIdx.x - at_tokens * n_cols;
+  const uint32_t bid = blockIdx.y * gridDim.x + blockIdx.x;        // (those past the last one: m0 >= M)
+  const int at_tokens = (int)(bid / n_cols), at_cols = (int)(bid % n_cols);
   const int m0 = (at_tokens * 4 + wave) * TOK, b0 = at_cols * 16;
   if (m0 >= g.M) return;
   const int k = b0 * MX4_BLOCK + lane * 8, left = g.K - k;         // values of the lane in front of K: left and more
@@ -200,11 +202,12 @@ hipError_t launch_quant_mx4(bool km, const QuantMx4Args& g, hipStream_t stream) 
   const bool few = km && values <= 1 << 21;
   const int64_t per = few ? 16 : km ? 128 : 4 * TOK;
   const int64_t n_tokens = (g.M + per - 1) / per, n_other = km ? (nb + 3) / 4 : (nb + 15) / 16;
-  if (n_tokens * n_other * 256 > 0xffffffffll) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(n_tokens * n_other));
+  // (2^27 row-major tokens of more than 512 values are more threads than one dimension takes)
+  const Grid2 n = grid_of((uint64_t)(n_tokens * n_other), 256);
+  const dim3 grid(n.x, n.y);
   if (few) return launch_kernel(quant_mx4_few_kernel, grid, dim3(256), stream, g, nb, (int)n_other);
   if (km) return launch_kernel(quant_mx4_km_kernel, grid, dim3(256), stream, g, nb, values < 8 << 20 ? (int)n_other : 0, (int)n_tokens);
-  return launch_kernel(quant_mx4_mk_kernel, grid, dim3(256), stream, g, nb, (int)n_other);
+  return launch_kernel(quant_mx4_mk_kernel, grid, dim3(256), stream, g, nb, (uint32_t)n_other);
 }
 
 }  // namespace twg

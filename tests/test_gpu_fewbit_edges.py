@@ -1,4 +1,5 @@
-"""Few-bit operators at the ends of what they allow: factors of the norm that are not finite (-m gpu)."""
+"""Few-bit operators at the ends of what they allow: factors of the norm that are not finite, the most values of a
+row-major quantiser (-m gpu)."""
 import numpy as np
 import pytest
 
@@ -75,3 +76,32 @@ def test_norm_with_factors_that_are_not_finite(M, K, residual, i8, f16):
             _assert_y(Y, y, K)
         if Q is not None:
             assert not Q.any() and np.isnan(s).all()
+
+def test_row_major_quantiser_of_the_most_tokens():
+    """2^27 row-major tokens of 520 values: more threads than one dimension of a grid takes."""
+    import torch
+    M, K, ldx, nb = 1 << 27, 520, 520, 17
+    if torch.cuda.mem_get_info()[0] < 190 << 30:
+        pytest.skip("needs 170 GiB of device memory")
+    dev = "cuda"
+    X = torch.zeros((M, ldx), dtype=torch.float16, device=dev)
+    Q = torch.full((nb, M, 16), 0xA5, dtype=torch.uint8, device=dev)
+    S = torch.full((nb, M), 0xA5, dtype=torch.uint8, device=dev)
+    rows = np.unique(np.concatenate([np.arange(20), (1 << 26) + np.arange(-17, 18), M - 1 - np.arange(40),
+                                     np.random.default_rng(1).integers(0, M, 200)]))
+    x = acts(4, rows.size, K)
+    at = torch.from_numpy(rows).to(dev)
+    X[at] = torch.from_numpy(x).to(dev)
+    print("row-major quantiser, 2^27 tokens of 520 values", flush=True)
+    tw.tw_quant_mx4(X.data_ptr(), M, K, ldx, tw.LAYOUT_MK, Q.data_ptr(), S.data_ptr(), M, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    codes, scale = ofb.mx4_quant(np.ascontiguousarray(x.T))
+    assert np.array_equal(Q[:, at].cpu().numpy(), ofb.mx4_bytes(codes))
+    assert np.array_equal(S[:, at].cpu().numpy(), scale)
+    for b in range(nb):                              # every other token is zeros
+        S[b, at] = 127
+        assert bool((S[b] == 127).all())
+        Q[b, at] = 0
+        assert not bool(Q[b].any())
+    del X, Q, S
+    torch.cuda.empty_cache()
