@@ -780,6 +780,7 @@ tw_status tw_gemm_i8_scaled(const void* A, int M, int lda, tw_handle_t h, const 
   if (!A || !C || !h || !a_scale || !w_scale || M < 1) return TW_ERR_ARG;
   if (!aligned16(A) || !aligned16(C) || lda % 16 || ldc % 8 || lda < M || ldc < M) return TW_ERR_ARG;
   if (((uintptr_t)a_scale & 3) || ((uintptr_t)w_scale & 3) || h->dtype != TW_DTYPE_I8) return TW_ERR_ARG;
+  if (M > MOST_TOKENS) return TW_ERR_UNSUPPORTED;
   if (!h->img.blob) return TW_ERR_STATE;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return TW_ERR_HIP;
