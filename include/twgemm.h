@@ -368,7 +368,8 @@ tw_status tw_conv_gemm_i8(const void* X_dev, tw_conv_t binding, void* C_dev, int
  * Common to the calls below: activations are K x M (token m of row k at X[k*ld + m], TW_LAYOUT_KM), device memory, 16-byte
  * aligned; the scales of tw_rmsnorm / tw_quant_i8 / tw_gemm_i8_scaled are 4-byte aligned.  Columns M .. ld-1 are never
  * written; they may be read (whatever they hold) and have to be readable (row-major input: values K .. ldx-1 of a row).
- * M <= 2^27 (the 4-bit calls: ldq <= 2^27) and K <= 131071, else TW_ERR_UNSUPPORTED.  Outputs must not overlap anything else (H_dev of tw_rmsnorm: see there); the address of
+ * M <= 2^27 (the 4-bit calls: ldq <= 2^27) and K <= 131071, else TW_ERR_UNSUPPORTED; products of 2^37 outputs and more, whose tiles
+ * can be more threads than a launch takes, may get it too.  Outputs must not overlap anything else (H_dev of tw_rmsnorm: see there); the address of
  * another operand as an output is TW_ERR_ARG.  Asynchronous on `stream`, allocate nothing, keep no state between calls.
  * Unlike elsewhere in this library an infinity or NaN is an allowed input of the norm and the quantisers: it marks its token
  * (its block of a token) as said there and reaches no other.
