@@ -508,11 +508,7 @@ __global__ __launch_bounds__(NWAVES * 64, (TM * TN >= 256 * 128) ? 2 : 1) void t
       if (cols[i] < 0 || m >= g.M) continue;
       int8_t* dst = (int8_t*)g.C + (size_t)cols[i] * g.ldc + m;
       if (m + 16 <= g.M) __builtin_nontemporal_store(pc[i], (int4v*)dst);
-      else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (m + e < g.M) dst[e] = (int8_t)(pc[i][e >> 2] >> (8 * (e & 3)));
-      }
+      else store_front(dst, (u32x4)pc[i], g.M & 15);
     }
   } else {
   // ---- epilogue, int32 output: stage as [n][m], half of the tile's columns at a time;

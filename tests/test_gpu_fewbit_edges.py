@@ -1,12 +1,15 @@
 """Few-bit operators at the ends of what they allow: factors of the norm that are not finite, the most values of a
-row-major quantiser (-m gpu)."""
+row-major quantiser, every number of tokens of an int8 output (-m gpu)."""
 import numpy as np
 import pytest
 
 import paper_2402_10876_amd as tw
 from oracle import fewbit as ofb
+from oracle import gemm as og
 from tests import fewbit_util as fu
 from tests.fewbit_util import acts, up
+from tests.helpers import random_tw_mask
+import workloads as wl
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +108,33 @@ def test_row_major_quantiser_of_the_most_tokens():
         assert not bool(Q[b].any())
     del X, Q, S
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("tile_m", [64, 128, 256])
+def test_int8_output_of_any_number_of_tokens(tile_m):
+    """The last piece of 16 tokens of a column holds 1 to 16 of them, for every height of the tiles and for weights of both
+    widths of tiles; the columns behind M are left as they were."""
+    import torch
+    rng = np.random.default_rng(5)
+    K, N = 140, 150
+    B = wl.rng_i8(K, (K, N))
+    for G in (64, 128):
+        mask = random_tw_mask(rng, K, N, G)
+        p = tw.tw_pack_i8(B, mask, G, tw.PATTERN_TW)
+        for M in range(497, 514):
+            A, ld = wl.rng_i8(M, (M, K)), up(M, 16) + 16
+            At = np.full((K, ld), 0x55, np.int8)
+            At[:, :M] = A.T
+            Ad = torch.from_numpy(At).cuda()
+            C = torch.full((N, ld), 99, dtype=torch.int8, device="cuda")
+            print(f"int8 output tile_m={tile_m} G={G} M={M}", flush=True)
+            tw.tw_set_option("tile_m", tile_m)
+            try:
+                tw.tw_gemm_i8(Ad.data_ptr(), M, ld, p, C.data_ptr(), ld, 1, 1e-3, torch.cuda.current_stream().cuda_stream)
+            finally:
+                tw.tw_set_option("tile_m", 0)
+            got = C.cpu().numpy()
+            sums = np.rint(A.astype(np.float64) @ (B * (mask != 0)).astype(np.float64))
+            assert np.array_equal(got[:, :M].T, og.requantize_i8(sums.astype(np.int64), 1e-3))
+            assert (got[:, M:] == 99).all()
+        p.free()
