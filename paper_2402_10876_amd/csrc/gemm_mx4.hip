@@ -329,27 +329,38 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 //   V  64 x 128 (1)   W  64 x 64 (1)   U  32 x 64 (1)   waves on their own: none waits for another
 //   P 128 x 128 (4)   wave tiles of 64 x 64
 //   S  32 x 32 (4 on shares of the list, 2 of a short one)   S2 64 x 32 (2 x 4)
-// R for long lists: 4096 x 4096, all, M = 8192 R 77, Q 95; half, R 46, Q 55; M = 4096 R 25.7, Q 28.6, V 28.4; M = 3100 24.8, 25.0, 24.3;
-// 1024 x 4096, all (16 steps), M = 8192 R 34.4, Q 35.5, M = 4096 16.8, 16.4; half (8 steps) 26.6, 24.6 and 14.8, 13.4; 8192 cubed
-// R 263.  Else by rounds: a CU holds 12 waves of W (1536 tiles of 64 x 128), 8 of V or 2 workgroups of Q (2048).  1024 x 4096, half, a
-// tenth of the columns pruned: M = 3100 (1421 tiles) W 12.1, V 12.7, Q 12.9; M = 4096 (1856) 15.0, 13.6, 13.3; M = 5000 (2291) 20.1,
-// 20.2, 19.8; M = 6000 (2726) 27.8, 23.8, 21.9; a quarter, M = 5000 14.3, 16.4, 16.3; 768 x 3000, half, M = 6000 (2068) 14.0, 17.3,
-// 17.7, M = 7000 (2420) 16.6, 18.5, 18.1, M = 8192 (2816) 21.8, 20.7, 20.9.  Long lists, few tiles: 4096 x 4096, half, M = 2500 V
-// 21.3, W 22.6, a quarter, M = 3100 15.8, 16.1.  Small ones: 1024 x 1024, half, M = 5000 (632) W 7.5, U 7.4, M = 3300 W 6.7, U 5.9,
-// P 6.4; 4096 x 4096, half, M = 1536 (768) W 14.3, U 17.7, P 16.3.  One round of P, long lists: 4096 x 4096, half, M = 1024 P 11.3, W
-// 12.6, U 13.1, 4096 x 2048, M = 1700 10.5, 12.4, 10.8; short ones 1024 x 4096, M = 1024 6.9, 7.2, 6.8.
-// Lists shared among waves where tiles of 64 rows would be fewer than 160 and a list is long: 4096 x 4096, half, M = 128
-// S2 5.2, S 6.0, U 7.6; all, M = 256 S2 10.5, U 12.0; 4096 x 1024, all, M = 512 S2 6.9, U 10; up to 256 tiles of S it has
-// the shortest way: 1024 x 1024, half, M = 256 S 3.0, S2 3.1, U 3.4; 4096 x 4096, M = 1 S 3.7, S2 4.3.  Shares of S: two, four
-// with 4 steps under way, four with 8: 1024 x 4096, half (8 steps), M = 1 3.0, 3.2, 3.5; 1024 x 1024, 16 experts, M = 64 4.5, 4.8, 5.5;
-// 2048 x 1024, 8 experts (16 steps), M = 256 5.1, 5.3, 5.9; 1536 x 672, half (about 14), M = 359 3.8, 3.6; 4096 x 4096, half (32), M = 32 4.1, 3.75, 3.6, all (64) 6.4, 5.4, 4.8.
-// By expert, where ranges end inside tiles (half kept): 2048 x 1024, 8 experts, M = 8192 W 13.1, V 14.4, U 15.2, Q 16.7, M = 6000 W
-// 11.2, U 12.1, M = 2048 U 7.2, W 8.3, M = 512 S 5.7, U 6.2; 1024 x 1024, 8 experts, M = 12000 V 12.7, W 13.7; 1024 x 4096, 8 experts,
-// M = 8192 V 33, W 37, Q 34; 4096 x 2048, 16 experts, M = 5000 V 32, W 39.  Few tokens each: 1024 x 1024, 32 experts, M = 4000 U 9.0, W
-// 9.7, M = 8000 U 12.4, W 12.2; 256 experts, M = 16384 V 48, U 50, W 55.
+// Tiles below are counted as 64 x 128, steps are of the longest list, half of the blocks kept unless said otherwise.
+// S, S2: lists shared among waves, where single waves would leave CUs idle.  Up to 12 steps S (two waves), to 1280 workgroups, with 4 steps
+// to 1024; S / U: 1024 x 1024, 8 steps, M = 1024 3.95 / 4.45, M = 1280 4.26 / 4.65, M = 1536 4.81 / 4.78; a quarter, 4 steps, M = 1024 3.53 /
+// 3.60, M = 1280 4.04 / 3.77; 1024 x 4096, 8 steps, M = 320 5.0 / 5.3, M = 384 5.7 / 5.4; S2 3.8 where S takes 3.4 (M = 512).  From 16 steps on
+// S2 to two workgroups a CU (128 tiles), S while it has one: S / S2 / U 2048 x 1024, M = 192 3.8 / 3.9 / 5.1, M = 1024 5.3 / 5.6 / 5.5, M = 1152
+// 5.6 / 7.1 / 5.7; 4096 x 4096, M = 128 6.0 / 5.2 / 7.3, M = 256 8.7 / 7.2 / 9.1; 8192 x 1024, M = 192 5.5 / 6.1 / 10.5, M = 1024 10.6 / 9.7 / 11.3,
+// M = 1152 11.9 / 12.3 / 11.3.  Shares of S: two, four with 4 steps under way, four with 8: 1024 x 4096, 8 steps, M = 1 3.0, 3.2, 3.5; 2048 x
+// 1024, 8 experts (16 steps), M = 256 5.1, 5.3, 5.9; 1536 x 672 (about 14), M = 359 3.8, 3.6; 4096 x 4096 (32), M = 32 4.1, 3.75, 3.6, all (64)
+// 6.4, 5.4, 4.8.
+// R: one workgroup a CU, so the last round has to be worth it.  One round from 384 tiles of 256 rows and 32 steps on: 4096 x 4096, M = 4096 R
+// 25.6, Q 29.0, V 29.1, M = 2560 23.1, 24.2, 21.3; 16 steps R 18.4, Q 18.5.  More rounds, 16 steps: 2048 x 4096, M = 4352 (32 tiles past the
+// first) R 28.6, Q 25.2, M = 5000 (128) 30.5, 29.7, M = 5400 (192) 30.1, 29.7, M = 5900 (256) 33.2, 35.0, M = 8704 (64 past the second) 43.5,
+// 40.7, M = 9216 (128) 43.4, 42.2, M = 10000 (256) 48.1, 53.4; 32 steps: 4096 x 4096, M = 4600 (64) 41.1, 38.5, M = 5000 (128) 42.7, 42.8, M =
+// 8704 (64 past the second) 63.6, 65.5; 64 steps: M = 4352 (32) 62, 64, M = 8192 77, 95; 8192 cubed R 263.
+// Q, V, W by rounds: a CU holds 12 waves of W (1536 tiles), 8 of V or 2 workgroups of Q (2048).  1024 x 4096, a tenth of the columns
+// pruned: M = 3100 (1421 tiles) W 12.1, V 12.7, Q 12.9; M = 4096 (1856) 15.0, 13.6, 13.3; M = 5000 (2291) 20.1, 20.2, 19.8; M = 6000
+// (2726) 27.8, 23.8, 21.9; nothing pruned M = 4992 (2496) W 19.0, Q 19.1, M = 5120 (2560) 19.8, 19.2; a quarter, M = 5000 14.3, 16.4, 16.3.
+// V from 16 steps on: 2048 x 4096, M = 2304 (1152) W 13.3, V 13.6, M = 2432 (1216) 14.0, 13.7, M = 3072 (1536) 18.1, 15.8.
+// P in one round, 16 steps and more: 4096 x 4096, M = 600 (160 tiles of 128 rows) P 10.2, U 10.3, M = 700 (192) 10.5, 11.3, M = 1024 (256) 11.3,
+// 13.2; 16 steps 7.5, 7.3; 7.8, 7.8; 8.3, 8.8; 8192 x 4096, M = 700 16.3, 18.2; short lists 1024 x 4096, M = 1024 6.9, U 6.8.
+// W from 640 tiles, long lists from the end of U's two waves a SIMD (512): 1024 x 1024, M = 4608 (576) W 7.1, U 6.8, M = 5120 (640) 7.25, 7.2,
+// M = 5632 7.6, 7.7; 2048 x 4096, M = 1088 (544) 9.4, 9.6; 4096 x 4096 13.3, 15.0.
+// By expert, where ranges end inside tiles (tiles: those of M tokens and one more for every expert).  S / U, 8 steps, to 1280 workgroups: 1024
+// x 1024, 8 experts, M = 800 (264 of 32 rows) 4.7 / 5.3, M = 1200 (360) 5.4 / 5.5, 32 experts, M = 700 (424) 6.7 / 6.7, 1024 x 2048, 8 experts, M
+// = 800 (528) 6.3 / 6.2; 16 steps, to 1024: 4 experts, M = 900 (256) 5.8 / 6.3, 32 experts, M = 300 (328) 8.4 / 8.1.  V, 8 steps, above 1240
+// tiles: 1024 x 2048, 4 experts, M = 4600 (1200) W 11.0, V 12.0, 16 experts, M = 4000 (1248) 15.1, 14.3, 8 experts of 1024 columns, M = 11500 (1496)
+// 17.2, 15.0; 16 steps, above 1100: 8 experts, M = 8192 (1088) 15.8, 16.3, M = 9000 (1184) 18.6, 17.2, 32 experts, M = 7000 (1128) 20.4,
+// 19.0; Q 0.7 to 2 us more than V.  W from 192 tokens an expert on: 8 experts, M = 6000 W 8.8, U 9.4, 16 experts, M = 5000 (16 steps) 13.2,
+// 13.8, 32 experts, M = 6000 13.4, 12.4, M = 7000 14.4, 14.1; 256 experts, M = 16384 V 48, U 50, W 55.
 // Tiles of 64 columns: no V by expert (512 x 3200, 5 experts, M = 6449 W 19.3, V 20.5; with 1024 x 4096 W 37, V 36), and U by two waves of
-// 32 x 32 while they are few and their lists short (640 x 270, half, M = 4735 4.3 against 4.6; 2048 x 1024, 8 experts, M = 2048, 16
-// steps 7.6 against 7.1).
+// 32 x 32 up to 600 tiles of 32 rows and short lists (640 x 512, M = 4000 (500) 4.3 against 4.4, M = 5000 (628) 4.9 and 5.0, M = 7000 (876) 5.7 and
+// 5.3; 2048 x 1024, 8 experts, M = 2048, 16 steps 7.6 against 7.1).
 template <int GB>
 static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
   const int64_t M = g.M, n = ((int64_t)g.n_tiles * GB + 3) / 4;        // column tiles of 128
@@ -359,18 +370,20 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
   if (g.offsets && M / g.n_members < 4096) {
     const int64_t met = g.n_members < M ? g.n_members : M, tiles64 = (M / 64 + met) * n;
     tiles32 = (M / 32 + met) * n;
-    if (tiles32 * 4 <= 1024) shape = S;
-    else if (GB == 4 && (tiles64 > 1536 || (tiles64 >= 1200 && steps >= 16))) shape = V;
+    if (tiles32 <= (steps < 16 ? 320 : 256)) shape = S;
+    else if (GB == 4 && tiles64 > (steps < 16 ? 1240 : 1100)) shape = V;
     else shape = tiles64 >= 640 && M / g.n_members >= 192 ? W : U;
   } else {
     auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
     tiles32 = tiles(32);
-    if (tiles(64) < 160 && (steps >= 16 || tiles(64) <= 48)) shape = M <= 32 || tiles32 * 4 <= 256 ? S : S2;
-    else if (tiles(256) >= 384 && steps >= (tiles(256) > 512 ? 16 : 32)) shape = R;
+    const int64_t t256 = tiles(256), past = t256 % 512;      // past: tiles of R (two of these) in its last round
+    const bool one_round = t256 <= 512;
+    if (steps < 16 ? tiles32 <= (steps > 4 ? 320 : 256) : tiles(64) <= 128) shape = steps < 16 || M <= 32 || tiles32 * 4 <= 256 ? S : S2;
+    else if (t256 >= 384 && (one_round ? steps >= 32 : steps >= 64 || (steps >= 32 ? t256 >= 640 : steps >= 16 && (past == 0 || past > 192)))) shape = R;
     else if (tiles(64) > 2450 || (tiles(64) > 1536 && (tiles(64) <= 2048 || steps >= 16))) shape = Q;
     else if (tiles(64) >= 1200 && steps >= 16) shape = V;
-    else if (steps >= 16 && tiles(128) >= 200 && tiles(128) <= 256) shape = P;
-    else shape = tiles(64) >= 640 ? W : U;
+    else if (steps >= 16 && tiles(128) > 160 && tiles(128) <= 256) shape = P;
+    else shape = tiles(64) >= 640 || (tiles(64) > 512 && steps >= 16) ? W : U;
   }
   if (shape == S) {
     if (steps <= 12) return launch_mx4<GB, 1, 1, 1, 1, 2, 4>(g, stream);

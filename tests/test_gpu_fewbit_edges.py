@@ -1,5 +1,6 @@
 """Few-bit operators at the ends of what they allow: factors of the norm that are not finite, the most values of a
-row-major quantiser, every number of tokens of an int8 output (-m gpu)."""
+row-major quantiser, every number of tokens of an int8 output, 4-bit products where the shape of the tiles changes
+(-m gpu)."""
 import numpy as np
 import pytest
 
@@ -138,3 +139,48 @@ def test_int8_output_of_any_number_of_tokens(tile_m):
             assert np.array_equal(got[:, :M].T, og.requantize_i8(sums.astype(np.int64), 1e-3))
             assert (got[:, M:] == 99).all()
         p.free()
+
+
+def _mx4(M, K, N, G, off=None):
+    """Products of 4-bit operands against the definition; off: the first tokens of every expert (the same weight for all)."""
+    import torch
+    rng = np.random.default_rng(M + K + N)
+    mask = fu.block_mask(rng, K, N, G, 0.95, 0.9)
+    B = (rng.standard_normal((K, N)) * 0.05).astype(np.float16)
+    X = acts(M, M, K)
+    X[M - 2, K // 3] = np.inf
+    stream = torch.cuda.current_stream().cuda_stream
+    Q, S = fu.quant_mx4_dev(tw, X, tw.LAYOUT_MK, stream)
+    p = tw.tw_pack_mx4(B, mask, G)
+    h = p if off is None else tw.tw_concat([p] * (len(off) - 1))
+    ldc = up(M, 8) + 8
+    C = torch.full((N, ldc), 7.0, dtype=torch.float16, device="cuda")
+    print(f"4-bit product M={M} K={K} N={N} G={G} off={off}", flush=True)
+    if off is None:
+        tw.tw_gemm_mx4(Q.data_ptr(), S.data_ptr(), M, Q.shape[1], h, C.data_ptr(), ldc, stream)
+    else:
+        o = torch.tensor(off, dtype=torch.int32, device="cuda")
+        tw.tw_gemm_mx4_grouped(Q.data_ptr(), S.data_ptr(), M, Q.shape[1], o.data_ptr(), h, C.data_ptr(), ldc, stream)
+    torch.cuda.synchronize()
+    got = C.cpu().numpy()
+    a, b = (0, M) if off is None else (off[0], off[-1])
+    assert (got[:, :a] == 7).all() and (got[:, b:] == 7).all()
+    codes, scale = ofb.mx4_quant(np.ascontiguousarray(X.T))
+    fu.assert_mx4_close(got[:, a:b], codes[:, a:b], scale[:, a:b], B, mask, G)
+
+
+@pytest.mark.parametrize("M,K,N,G", [
+    (1000, 500, 1000, 128), (1500, 500, 1000, 128), (900, 200, 1000, 128), (1300, 200, 1000, 128),      # short lists: shared or single waves
+    (1000, 2000, 1000, 128), (1150, 2000, 1000, 64), (3000, 300, 500, 64), (5000, 300, 500, 64),        # long ones; pairs of waves
+    (3100, 2100, 4000, 128), (8199, 1030, 2200, 128), (12001, 1030, 2200, 128), (5400, 2100, 4000, 128),  # one round, one barely begun, more
+    (700, 1100, 4000, 128), (610, 1100, 4000, 128), (1090, 1100, 4000, 128), (4700, 500, 1000, 128)])
+def test_4_bit_products_where_tile_shapes_change(M, K, N, G):
+    _mx4(M, K, N, G)
+
+
+@pytest.mark.parametrize("K,N,G,off", [
+    (500, 1000, 128, [0, 100, 100, 350, 600, 610, 700, 790, 803]), (500, 1000, 128, [1, 300, 301, 700, 1201]),
+    (300, 500, 64, [0, 700, 1500, 1501, 3001]), (1100, 1000, 128, [0, 1000, 2500, 2501, 5000, 6000, 7700, 8000, 9000]),
+    (300, 2000, 128, [5, 1300, 2600, 3900, 5301]), (1030, 2200, 128, [5, 6001, 12010])])
+def test_4_bit_products_by_expert_where_tile_shapes_change(K, N, G, off):
+    _mx4(off[-1] + 3, K, N, G, off)
