@@ -39,7 +39,6 @@ struct GemmMx4Args {
   const uint8_t *vals, *wscale;
   int list_len;                  // entries of `blocks` per tile
   int n_tiles;                   // grouped: of a member
-  int n_mtiles;
   const int32_t* offsets;        // grouped: n_members + 1 first tokens, else null
   int n_members, member_n;       // grouped: columns of a member
 };

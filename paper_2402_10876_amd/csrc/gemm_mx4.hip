@@ -317,11 +317,9 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
   }
   const int64_t grid = mtiles * g.n_tiles * SUB;
   if (grid * (64 * WM * WN * WK) > 0xffffffffll) return hipErrorInvalidValue;
-  g.n_mtiles = (int)mtiles;
   return launch_kernel(gemm_mx4_kernel<GB, MB, NB, WM, WN, WK, D>, dim3((unsigned)grid), dim3(64 * WM * WN * WK), stream, g);
 }
 
-#ifndef TUNE
 // Tile shapes, tokens x columns (waves), us per launch in a captured stream of launches, operands from HBM, K x N and
 // the share of the blocks kept:
 //   R 512 x 128 (4)   wave tiles of 128 x 128: one read of the caches per 16 matrix instructions
@@ -408,6 +406,5 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
 hipError_t launch_gemm_mx4(int G, GemmMx4Args g, hipStream_t stream) {
   return G == 128 ? dispatch_mx4<4>(g, stream) : dispatch_mx4<2>(g, stream);
 }
-#endif
 
 }  // namespace twg

@@ -6,11 +6,13 @@
 //
 // inv cancels in q, which is therefore exact: u = fma(g, fl(127 / max|g|), 1.5 * 2^23) rounds to an integer in the low byte of
 // u, wrong only within 127 * 2^-24 of a half; where the distance to n is more than 0.49998 the side is settled in 64 bits
-// (254 g against (2n +- 1) max|g|, both exact).  Sums of squares are fp32 (at most 32 terms a lane, then a tree).
+// (254 g against (2n +- 1) max|g|, both exact).  Sums of squares are fp32: at most ceil(K / 128)
+// terms in a row, then a tree and 16 waves.
 //
 // Bound by memory: 2 bytes in per value (4 with a residual), 1 to 5 out.  One workgroup owns 8 to 64 tokens and all K rows and
 // keeps its values in registers (and LDS) between the two passes, up to 16 rows a lane; longer columns are read again, from L2.
-// Many long tokens with a residual go in slices of their rows (below).
+// Tokens of more than 8192 rows go in slices of their rows (below), shorter ones where that was measured to be faster, the int8
+// quantiser's as well as the norm's (slices_pay).
 #include <type_traits>
 
 #include "device_common.h"
@@ -605,7 +607,6 @@ hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
   return e;
 }
 
-#ifndef TUNE
 // Tokens per workgroup: 8 while that is at most one workgroup per CU (few rows of a token per lane and every CU at
 // work), 16 up to two, then 32, whose pieces of a row are half a line of memory; above 16384 whole lines.
 // Rows in registers as far as they fit, fewer lanes where they would have nothing to do.  us with 8 / 16 / 32 / 64 tokens, int8
@@ -640,6 +641,5 @@ static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
 hipError_t launch_norm(bool norm, const NormArgs& g, hipStream_t stream) {
   return norm ? dispatch_norm<true>(g, stream) : dispatch_norm<false>(g, stream);
 }
-#endif
 
 }  // namespace twg
