@@ -364,18 +364,22 @@ hipError_t run_norm(const NormArgs& g, hipStream_t stream) {
 // few workgroups.  With long tokens three launches on 128 tokens x one slice of the rows are faster, every access whole lines: sums of
 // the slices (and H), sums of the tokens, outputs.  No memory beyond the outputs is used: between the launches the sums of a slice,
 // 8 bytes per token, lie in the first rows of that slice of Q (8 rows of bytes; of Y 4 rows of halves without Q), which the last
-// launch reads before it writes them.  us, one launch / three, from HBM, residual and int8 output: 4096 rows, 32 tokens 9.8 / 10.5, 64
-// tokens 14.7 / 10.7, 512 tokens 17.7 / 13.2, 8192 tokens 79 / 65.6; 2500 rows, 64 tokens 10.8 / 10.8, 1024 tokens 14.0 / 13.7; 8192
-// rows, 16 tokens 12.0 / 12.2, 256 tokens 32 / 14.5; 16384 rows, 8 tokens 68 / 16; 2048 rows, 1024 tokens 11.8 / 12.8, 8192 tokens
-// 40.8 / 36.8; 1024 rows, 8192 tokens 20.9 / 24.5, 16384 tokens 38.2 / 36.7.  Without a residual: 4096 rows, 8192 tokens 41.8 / 42.9,
-// with both outputs 62.7 / 55.4; 6000 rows, 64 tokens 11.5 / 11.6, 8192 tokens 60.7 / 59.8; 8192 rows, 64 tokens 14.5 / 12.0, 8192
-// tokens 88 / 76.  (Of 8 rows a lane in workgroups of 256 threads 72 where 2 rows in 1024 threads take 65.6.)
+// launch reads before it writes them.  us, one launch / three, from HBM (600 MB of buffers in turn), residual and int8 output: 4096 rows, 32
+// tokens 9.7 / 11.0, 64 tokens 14.4 / 11.5, 512 tokens 26 / 13.9 (from the last-level cache 18.0 / 12.8), 8192 tokens 81 / 66; 2500 rows, 64
+// tokens 10.5 / 11.2, 1024 tokens 18.2 / 14.5; 8192 rows, 16 tokens 11.5 / 12.6, 256 tokens 42 / 15.2; 16384 rows, 8 tokens 68 / 16;
+// 2048 rows, 1024 tokens 14.1 / 13.6 (11.2 / 12.5), 8192 tokens 40.7 / 37.5; 1024 rows, 8192 tokens 20.2 / 23.9, 16384 tokens 37.5 / 36.3.
+// Without a residual: 4096 rows, 8192 tokens 40.9 / 43.1, with both outputs 63 / 55; 6000 rows, 64 tokens 11.1 / 11.9, 8192 tokens 60.3 /
+// 59.7; 8192 rows, 64 tokens 14.1 / 12.3, 8192 tokens 86 / 76.  (Of 8 rows a lane in workgroups of 256 threads 72 where 2 rows in
+// 1024 threads take 65.6.)
 constexpr int SL_TOK = 128, SL_NT = 1024, SL_RPP = SL_NT / (SL_TOK / 8), SL_CH = 2;      // 64 rows at a time, twice
 constexpr int SL_ROWS = SL_CH * SL_RPP;
 
+static bool slices_fit(const NormArgs& g) {              // threads of a grid
+  return (((int64_t)g.M + SL_TOK - 1) / SL_TOK) * ((g.K + SL_ROWS - 1) / SL_ROWS) * SL_NT <= 0xffffffffll;
+}
 static bool slices_pay(const NormArgs& g) {
   const int64_t values = (int64_t)g.M * g.K;
-  if ((((int64_t)g.M + SL_TOK - 1) / SL_TOK) * ((g.K + SL_ROWS - 1) / SL_ROWS) * SL_NT > 0xffffffffll) return false;      // threads of a grid
+  if (!slices_fit(g)) return false;
   if (g.K > 8192) return true;
   if (g.R) return g.K > 2048 ? values >= 160000 : g.K >= 1024 && values >= 1 << 24;
   return g.K > 4096 ? values >= 400000 : g.K > 2048 && g.Y && g.Q && values >= 1 << 24;
@@ -608,11 +612,14 @@ hipError_t run_norm_slices(const NormArgs& g, int n, hipStream_t stream) {
 }
 
 // Tokens per workgroup: 8 while that is at most one workgroup per CU (few rows of a token per lane and every CU at
-// work), 16 up to two, then 32, whose pieces of a row are half a line of memory; above 16384 whole lines.
-// Rows in registers as far as they fit, fewer lanes where they would have nothing to do.  us with 8 / 16 / 32 / 64 tokens, int8
-// output, from HBM, with a residual: 768 rows, 2048 tokens 6.8 / 7.3 / 8.7, 4096 tokens 11.8 / 9.2 / 11.0; 1024 rows, 8192 tokens
-// 30 / 25 / 21 / 28; 4096 rows, 16 tokens 6.8 / 9.8 / 20, 512 tokens 17 / 23 / 35.  Without: 4096 rows, 1024 tokens 11.3 / 13.7 /
-// 20, 4096 tokens 28 / 23 / 32, 8192 tokens 51 / 46 / 42 / 47, 16384 tokens - / 91 / 90 / 77.
+// work), 16 up to two, then 32, whose pieces of a row are half a line of memory; where a workgroup fills a CU (above 2048
+// rows) 32 for one round, whole lines for one round, then slices (not up to 2560 rows where the last round is well filled).  Rows in registers as far as they fit, fewer lanes where they would have
+// nothing to do.  us with 8 / 16 / 32 / 64 tokens, int8 output, from HBM (600 MB of buffers in turn), with a residual: 768 rows, 2048 tokens
+// 7.7 / 9.8 / 11.9 / 19, 4096 tokens 13.3 / 11.4 / 13.5 / 20, 6000 tokens 19.7 / 17.3 / 14.8 / 23; 1024 rows, 8192 tokens 29 / 24 / 20 / 27; 2048
+// rows, 2500 tokens 26 / 20 / 26 / 41; 4096 rows, 16 tokens 7.1 / 9.5 / 20 / 36 (buffers that the last-level cache holds: 768 rows, 4096
+// tokens 10.8 / 8.2 / 9.5).  Without: 4096 rows, 1024 tokens 13.4 / 17.9 / 27 / 39, 4096 tokens 29 / 23 / 33 / 44, 8192 tokens 50 / 45 / 41 / 47,
+// 9000 tokens 66 / 57 / 72 / 57 (slices 56), 16000 tokens 97 / 75 / 72 / 72 (75), 17000 tokens 120 / 96 / 115 / 124 (95); 2100 rows, 9000
+// tokens 35 / 33 / 43 / 34 (35), 16000 tokens 52 / 46 / 43 / 34 (45), 18000 tokens 63 / 57 / 71 / 72 (58), 24000 tokens 73 / 64 / 63 / 60 (62).
 template <bool NORM>
 static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   const int K = g.K;
@@ -631,10 +638,15 @@ static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   if (g.M < 1 << 25) {                   // (2^32 threads in a grid: none of 32 tokens beyond 2^27 - 1)
     if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
     if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
-    // half of the rows in LDS: the quantiser, 8192 x 4096, 36 us against 42 read again; the norm spills registers there
+    // Half of the rows in LDS: the quantiser, 8192 tokens x 4096, 35 us against 41 read again and 41 in slices (a copy 19.5: all
+    // of a workgroup's loads come before its stores, and its 128 KiB of LDS leave a CU no second one; the stores are pieces of
+    // 32 bytes); 17000 tokens 87, 108, 92.  The norm spills registers there.
     if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);
-    if (g.M <= 16384 - 64) return run_norm<NORM, 32, 1024, 0>(g, stream);
+    if constexpr (NORM)
+      if (g.M <= 8192) return run_norm<NORM, 32, 1024, 0>(g, stream);
   }
+  if (K > 2048 && g.M > 16384 && (K > 2560 || g.M % 16384 < 6144) && slices_fit(g))
+    return run_norm_slices<NORM>(g, (K + SL_ROWS - 1) / SL_ROWS, stream);
   return run_norm<NORM, 64, 1024, 0>(g, stream);
 }
 

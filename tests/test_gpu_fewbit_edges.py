@@ -51,9 +51,9 @@ def _assert_y(got, y, K):
     assert (err <= size * (fu.STEP16 + fu.norm_tol(K)) * (1 + fu.STEP16) + 2.0 ** -25).all()
 
 
-# One launch that keeps its rows, one that reads them again (2050 rows of 4100 and 16400 tokens without a residual), slices.
+# One launch that keeps its rows, one that reads them again (2050 rows of 4100, 8200 and 16384 tokens without a residual), slices.
 @pytest.mark.parametrize("M,K,residual", [(1, 1, False), (40, 5, True), (40, 1500, False), (33, 1003, True), (3000, 700, True),
-                                          (4100, 300, False), (4100, 2050, False), (16400, 2049, False), (16450, 96, True),
+                                          (4100, 300, False), (4100, 2050, False), (8200, 2050, False), (16384, 2049, False), (16400, 2049, False), (24001, 2050, False), (16450, 96, True),
                                           (70, 4200, True), (1030, 2100, True), (100, 6000, False), (3, 8200, False), (5, 8200, True)])
 @pytest.mark.parametrize("i8,f16", [(False, True), (True, True), (True, False)])
 def test_norm_with_factors_that_are_not_finite(M, K, residual, i8, f16):
