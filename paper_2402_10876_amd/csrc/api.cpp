@@ -705,6 +705,10 @@ tw_status tw_dense_gemm(const void* A, const void* B, void* C, int M, int K, int
 //   256 rows where they are one round and 128 rows are not (128 / 256 rows: 4096 x 4096 at 50 %, M = 4096 50.5 / 32.9 and
 //   47.5 / 31.8; 1024 x 4096 at 50 % 19.1 / 15.2 and 14.9 / 13.3; 768 x 2304 at 75 %, M = 6000 16.7 / 13.6 and 12.3 / 11.0; with
 //   one round of 128 rows 768 x 2304, M = 4096 8.0 / 9.6, with two of 256 M = 8192 14.0 / 18.1).
+//   Convolutions go by the same rule (int8 / int32 output; 64 / 128 rows: 512 -> 512, 3 x 3 at 14 x 14, batch 8, 90 % 6.2 / 7.3 and 6.7 /
+//   8.0; 512 -> 512, 3 x 3 at 28 x 28, 87.5 % 8.7 / 8.8 and 8.3 / 9.0; 64 -> 64, 3 x 3 at 56 x 56, 50 % 6.2 / 6.0 and 5.9 / 6.0; 128 / 256 rows:
+//   256 -> 1024, 3 x 3 at 28 x 28, batch 16, 75 % 19.4 / 18.5 and 25.0 / 20.0; 128 -> 128, 3 x 3 at 112 x 112, batch 8, 87.5 % 12.4 /
+//   11.5 and 18.5 / 14.7; 64 -> 256, 1 x 1 at 56 x 56, batch 16, 50 % 9.1 / 8.4 and 13.6 / 12.8).
 // The dense baseline measured worse with 64 rows.
 static int pick_tile_m_i8(const Opts& o, int M, int n_tiles, int G, int max_k, bool dense) {
   const int forced = o.tile_m;

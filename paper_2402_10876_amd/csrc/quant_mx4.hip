@@ -9,8 +9,8 @@
 //   M x K : a wave takes 16 blocks of 4 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
 //           collected in LDS so that the writes are runs of 64 bytes (4 tokens of a block row).  Workgroups that start
 //           together read whole tokens: side by side down the rows they meet the same channels of memory where a row
-//           is a power of two of bytes.  us, tokens first / whole tokens: 8192 x 4096 19.8 / 17.3 (floor 16.5), 8192 x 2048 10.3 /
-//           8.1, 4096 x 768 3.7 / 3.6; of 8 tokens 20.9 / 18.0, and one token of 4096 values 2.7 against 2.35.
+//           is a power of two of bytes.  us, tokens first / whole tokens: 8192 x 4096 20.0 / 17.2 (a copy 16.5), 8192 x 2048 12.2 / 10.5 (8.2;
+//           from the last-level cache 10.2 / 7.9), 8192 x 1024 6.5 / 6.5, 4096 x 768 4.5 / 4.4; waves of 8 tokens 8192 x 4096 20.9 / 18.0.
 #include <type_traits>
 
 #include "device_common.h"
@@ -63,7 +63,7 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
 }  // namespace
 
 // K x M.  One wave: 128 tokens x one block of rows; neighbouring workgroups along the rows (n_rows of them) or along the tokens.
-// us along rows / tokens: 4096 x 768 3.5 / 3.9, 1957 x 1003 3.0 / 3.4, 5000 x 1003 4.7 / 5.2, 8192 x 1024 5.5 / 5.5, 8192 x 4096 20.7 / 20.0.
+// us along rows / tokens, from HBM: 4096 x 768 4.3 / 4.2, 5000 x 1003 5.35 / 5.8, 8192 x 1024 6.5 / 6.4, 8192 x 4096 20.7 / 19.8.
 __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n_blocks, int n_rows, int n_tokens) {
   const int lane = threadIdx.x & 63;
   const int bid = (int)(blockIdx.y * gridDim.x + blockIdx.x);      // (those past the last one: no block or no token)
@@ -100,7 +100,8 @@ __global__ __launch_bounds__(256) void quant_mx4_km_kernel(QuantMx4Args g, int n
 }
 
 // K x M, few values.  One wave: 16 tokens x one block of rows; a lane takes two tokens and 4 rows.  us, 32 rows a lane / 4 rows: 1 x
-// 4096 3.7 / 2.2, 16 x 4096 4.2 / 2.3, 128 x 1024 2.9 / 2.3, 1024 x 1024 3.0 / 2.6, 2048 x 1024 3.1 / 2.9, 4096 x 768 3.6 / 6.0.
+// 4096 3.4 / 1.9, 16 x 4096 3.9 / 2.0, 128 x 1024 2.6 / 2.0, 1024 x 1024 3.15 / 2.75, 1957 x 1003 3.8 / 3.5, 2048 x 1024 3.75 / 4.1, 4096 x 768
+// 4.25 / 6.5.
 __global__ __launch_bounds__(256) void quant_mx4_few_kernel(QuantMx4Args g, int n_blocks, int n_rows) {
   const int lane = threadIdx.x & 63, pair = lane & 7, part = lane >> 3;
   const int at_tokens = (int)blockIdx.x / n_rows, at_rows = (int)blockIdx.x - at_tokens * n_rows;
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(256) void quant_mx4_mk_kernel(QuantMx4Args g, int n
 hipError_t launch_quant_mx4(bool km, const QuantMx4Args& g, hipStream_t stream) {
   const int nb = (g.K + MX4_BLOCK - 1) / MX4_BLOCK;
   const int64_t values = (int64_t)g.M * g.K;
-  const bool few = km && values <= 1 << 21;
+  const bool few = km && values < 1 << 21;
   const int64_t per = few ? 16 : km ? 128 : 4 * TOK;
   const int64_t n_tokens = (g.M + per - 1) / per, n_other = km ? (nb + 3) / 4 : (nb + 15) / 16;
   // (2^27 row-major tokens of more than 512 values are more threads than one dimension takes)
