@@ -638,7 +638,7 @@ static hipError_t dispatch_norm(const NormArgs& g, hipStream_t stream) {
   if (g.M < 1 << 25) {                   // (2^32 threads in a grid: none of 32 tokens beyond 2^27 - 1)
     if (K <= 1024) return run_norm<NORM, 32, 1024, 4>(g, stream);
     if (K <= 2048) return run_norm<NORM, 32, 1024, 8>(g, stream);
-    // Half of the rows in LDS: the quantiser, 8192 tokens x 4096, 35 us against 41 read again and 41 in slices (a copy 19.5: all
+    // Half of the rows in LDS: the quantiser, 8192 tokens x 4096, 35 us against 41 read again and 41 in slices (a copy 18.3: all
     // of a workgroup's loads come before its stores, and its 128 KiB of LDS leave a CU no second one; the stores are pieces of
     // 32 bytes); 17000 tokens 87, 108, 92.  The norm spills registers there.
     if (!NORM && K <= 4096) return run_norm<NORM, 32, 1024, 8, 8>(g, stream);

@@ -9,7 +9,7 @@
 //   M x K : a wave takes 16 blocks of 4 tokens, 1 KiB of a token per load; four lanes hold a block, whose codes are
 //           collected in LDS so that the writes are runs of 64 bytes (4 tokens of a block row).  Workgroups that start
 //           together read whole tokens: side by side down the rows they meet the same channels of memory where a row
-//           is a power of two of bytes.  us, tokens first / whole tokens: 8192 x 4096 20.0 / 17.2 (a copy 16.5), 8192 x 2048 12.2 / 10.5 (8.2;
+//           is a power of two of bytes.  us, tokens first / whole tokens: 8192 x 4096 20.0 / 17.2 (a copy 15.4), 8192 x 2048 12.2 / 10.5 (7.7;
 //           from the last-level cache 10.2 / 7.9), 8192 x 1024 6.5 / 6.5, 4096 x 768 4.5 / 4.4; waves of 8 tokens 8192 x 4096 20.9 / 18.0.
 #include <type_traits>
 
