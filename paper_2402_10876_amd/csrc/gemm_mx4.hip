@@ -328,8 +328,8 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 //   P 128 x 128 (4)   wave tiles of 64 x 64
 //   S  32 x 32 (4 on shares of the list, 2 of a short one)   S2 64 x 32 (2 x 4)
 // Tiles below are counted as 64 x 128, steps are of the longest list, half of the blocks kept unless said otherwise.
-// S, S2: lists shared among waves, where single waves would leave CUs idle.  Up to 12 steps S (two waves), to 1280 workgroups, with 4 steps
-// to 1024; S / U: 1024 x 1024, 8 steps, M = 1024 3.95 / 4.45, M = 1280 4.26 / 4.65, M = 1536 4.81 / 4.78; a quarter, 4 steps, M = 1024 3.53 /
+// S, S2: lists shared among waves, where single waves would leave CUs idle.  Up to 12 steps S (two waves), to 1280 workgroups, with 4 steps or
+// tiles of 64 columns to 1024; S / U: 1024 x 1024, 8 steps, M = 1024 3.95 / 4.45, M = 1280 4.26 / 4.65, M = 1536 4.81 / 4.78; a quarter, 4 steps, M = 1024 3.53 /
 // 3.60, M = 1280 4.04 / 3.77; 1024 x 4096, 8 steps, M = 320 5.0 / 5.3, M = 384 5.7 / 5.4; S2 3.8 where S takes 3.4 (M = 512).  From 16 steps on
 // S2 to two workgroups a CU (128 tiles), S while it has one: S / S2 / U 2048 x 1024, M = 192 3.8 / 3.9 / 5.1, M = 1024 5.3 / 5.6 / 5.5, M = 1152
 // 5.6 / 7.1 / 5.7; 4096 x 4096, M = 128 6.0 / 5.2 / 7.3, M = 256 8.7 / 7.2 / 9.1; 8192 x 1024, M = 192 5.5 / 6.1 / 10.5, M = 1024 10.6 / 9.7 / 11.3,
@@ -345,15 +345,16 @@ static hipError_t launch_mx4(GemmMx4Args g, hipStream_t stream) {
 // pruned: M = 3100 (1421 tiles) W 12.1, V 12.7, Q 12.9; M = 4096 (1856) 15.0, 13.6, 13.3; M = 5000 (2291) 20.1, 20.2, 19.8; M = 6000
 // (2726) 27.8, 23.8, 21.9; nothing pruned M = 4992 (2496) W 19.0, Q 19.1, M = 5120 (2560) 19.8, 19.2; a quarter, M = 5000 14.3, 16.4, 16.3.
 // V from 16 steps on: 2048 x 4096, M = 2304 (1152) W 13.3, V 13.6, M = 2432 (1216) 14.0, 13.7, M = 3072 (1536) 18.1, 15.8.
-// P in one round, 16 steps and more: 4096 x 4096, M = 600 (160 tiles of 128 rows) P 10.2, U 10.3, M = 700 (192) 10.5, 11.3, M = 1024 (256) 11.3,
-// 13.2; 16 steps 7.5, 7.3; 7.8, 7.8; 8.3, 8.8; 8192 x 4096, M = 700 16.3, 18.2; short lists 1024 x 4096, M = 1024 6.9, U 6.8.
-// W from 640 tiles, long lists from the end of U's two waves a SIMD (512): 1024 x 1024, M = 4608 (576) W 7.1, U 6.8, M = 5120 (640) 7.25, 7.2,
+// P in one round, above 160 tiles of 128 rows, up to 28 steps above 192: 4096 x 4096, M = 600 (160) P 10.2, U 10.3, M = 700 (192) 10.5, 11.3, M = 1024 (256) 11.3,
+// 13.2; 16 steps 7.5, 7.3; 7.8, 7.8; 8.3, 8.8; 20 steps 2041 x 3616, M = 822 (182) 9.6, 9.2; 8192 x 4096, M = 700 16.3, 18.2; short lists 1024 x 4096, M = 1024 6.9, U 6.8.
+// W from 640 tiles, from 24 steps on from the end of U's two waves a SIMD (512): 1024 x 1024, M = 4608 (576) W 7.1, U 6.8, M = 5120 (640) 7.25, 7.2,
 // M = 5632 7.6, 7.7; 2048 x 4096, M = 1088 (544) 9.4, 9.6; 4096 x 4096 13.3, 15.0.
-// By expert, where ranges end inside tiles (tiles: those of M tokens and one more for every expert).  S / U, 8 steps, to 1280 workgroups: 1024
+// By expert, where ranges end inside tiles (tiles: those of M tokens and one more for every expert).  S / U, 8 steps, to 1280 workgroups as above: 1024
 // x 1024, 8 experts, M = 800 (264 of 32 rows) 4.7 / 5.3, M = 1200 (360) 5.4 / 5.5, 32 experts, M = 700 (424) 6.7 / 6.7, 1024 x 2048, 8 experts, M
 // = 800 (528) 6.3 / 6.2; 16 steps, to 1024: 4 experts, M = 900 (256) 5.8 / 6.3, 32 experts, M = 300 (328) 8.4 / 8.1.  V, 8 steps, above 1240
 // tiles: 1024 x 2048, 4 experts, M = 4600 (1200) W 11.0, V 12.0, 16 experts, M = 4000 (1248) 15.1, 14.3, 8 experts of 1024 columns, M = 11500 (1496)
-// 17.2, 15.0; 16 steps, above 1100: 8 experts, M = 8192 (1088) 15.8, 16.3, M = 9000 (1184) 18.6, 17.2, 32 experts, M = 7000 (1128) 20.4,
+// 17.2, 15.0; 4 steps, above 1536: 96 x 1024, 8 experts, M = 11000 (1432) 8.8, 10.0, M =
+// 12500 (1624) 11.6, 10.5; 16 steps, above 1100: 8 experts, M = 8192 (1088) 15.8, 16.3, M = 9000 (1184) 18.6, 17.2, 32 experts, M = 7000 (1128) 20.4,
 // 19.0; Q 0.7 to 2 us more than V.  W from 192 tokens an expert on: 8 experts, M = 6000 W 8.8, U 9.4, 16 experts, M = 5000 (16 steps) 13.2,
 // 13.8, 32 experts, M = 6000 13.4, 12.4, M = 7000 14.4, 14.1; 256 experts, M = 16384 V 48, U 50, W 55.
 // Tiles of 64 columns: no V by expert (512 x 3200, 5 experts, M = 6449 W 19.3, V 20.5; with 1024 x 4096 W 37, V 36), and U by two waves of
@@ -365,23 +366,24 @@ static hipError_t dispatch_mx4(const GemmMx4Args& g, hipStream_t stream) {
   const int steps = g.list_len / 2;
   enum { R, Q, P, V, W, U, S, S2 } shape;
   int64_t tiles32;
+  const int short_most = GB == 4 && steps > 4 && steps < 16 ? 320 : 256;
   if (g.offsets && M / g.n_members < 4096) {
     const int64_t met = g.n_members < M ? g.n_members : M, tiles64 = (M / 64 + met) * n;
     tiles32 = (M / 32 + met) * n;
-    if (tiles32 <= (steps < 16 ? 320 : 256)) shape = S;
-    else if (GB == 4 && tiles64 > (steps < 16 ? 1240 : 1100)) shape = V;
+    if (tiles32 <= short_most) shape = S;
+    else if (GB == 4 && tiles64 > (steps >= 16 ? 1100 : steps > 4 ? 1240 : 1536)) shape = V;
     else shape = tiles64 >= 640 && M / g.n_members >= 192 ? W : U;
   } else {
     auto tiles = [&](int rows) { return (M + rows - 1) / rows * n; };
     tiles32 = tiles(32);
     const int64_t t256 = tiles(256), past = t256 % 512;      // past: tiles of R (two of these) in its last round
     const bool one_round = t256 <= 512;
-    if (steps < 16 ? tiles32 <= (steps > 4 ? 320 : 256) : tiles(64) <= 128) shape = steps < 16 || M <= 32 || tiles32 * 4 <= 256 ? S : S2;
+    if (steps < 16 ? tiles32 <= short_most : tiles(64) <= 128) shape = steps < 16 || M <= 32 || tiles32 * 4 <= 256 ? S : S2;
     else if (t256 >= 384 && (one_round ? steps >= 32 : steps >= 64 || (steps >= 32 ? t256 >= 640 : steps >= 16 && (past == 0 || past > 192)))) shape = R;
     else if (tiles(64) > 2450 || (tiles(64) > 1536 && (tiles(64) <= 2048 || steps >= 16))) shape = Q;
     else if (tiles(64) >= 1200 && steps >= 16) shape = V;
-    else if (steps >= 16 && tiles(128) > 160 && tiles(128) <= 256) shape = P;
-    else shape = tiles(64) >= 640 || (tiles(64) > 512 && steps >= 16) ? W : U;
+    else if (steps >= 16 && tiles(128) > (steps >= 32 ? 160 : 192) && tiles(128) <= 256) shape = P;
+    else shape = tiles(64) >= 640 || (tiles(64) > 512 && steps >= 24) ? W : U;
   }
   if (shape == S) {
     if (steps <= 12) return launch_mx4<GB, 1, 1, 1, 1, 2, 4>(g, stream);

@@ -174,7 +174,8 @@ def _mx4(M, K, N, G, off=None):
     (1000, 500, 1000, 128), (1500, 500, 1000, 128), (900, 200, 1000, 128), (1300, 200, 1000, 128),      # short lists: shared or single waves
     (1000, 2000, 1000, 128), (1150, 2000, 1000, 64), (3000, 300, 500, 64), (5000, 300, 500, 64),        # long ones; pairs of waves
     (3100, 2100, 4000, 128), (8199, 1030, 2200, 128), (12001, 1030, 2200, 128), (5400, 2100, 4000, 128),  # one round, one barely begun, more
-    (700, 1100, 4000, 128), (610, 1100, 4000, 128), (1090, 1100, 4000, 128), (4700, 500, 1000, 128)])
+    (700, 1100, 4000, 128), (900, 1100, 4000, 128), (700, 2100, 4000, 128), (1090, 1100, 4000, 128), (1090, 2100, 4000, 128),
+    (4700, 500, 1000, 128)])
 def test_4_bit_products_where_tile_shapes_change(M, K, N, G):
     _mx4(M, K, N, G)
 
